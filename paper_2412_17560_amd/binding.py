@@ -28,6 +28,11 @@ class _Info(C.Structure):
                 ("reserved0", C.c_int32)]
 
 
+class _CacheInfo(C.Structure):
+    _fields_ = [("n_pages", C.c_int64), ("page_tokens", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("token_bytes", C.c_int32), ("device_bytes", C.c_int64), ("workspace_bytes", C.c_int64)]
+
+
 def library_path() -> str:
     return _build.LIB
 
@@ -103,6 +108,23 @@ def _lib():
     lib.gqsa_copy.argtypes = [vp, vp, C.c_size_t, vp]
     lib.gqsa_launch_floor.restype = C.c_int
     lib.gqsa_launch_floor.argtypes = [i32, i32, vp, vp]
+    heads = [vp, i64, i64]                               # an array [rows, heads, head_dim]: pointer, distances
+    sequences = [vp, i32, vp, vp, i32]                   # pages, max_pages, lengths, row_starts, n_seqs
+    lib.gqsa_qk_norm_rotate.restype = C.c_int
+    lib.gqsa_qk_norm_rotate.argtypes = [*heads, i32, *heads, i32, i64, i32, vp, vp, C.c_float, vp, i64, i32, i32, vp, *heads, *heads, vp]
+    lib.gqsa_cache_create.restype = C.c_int
+    lib.gqsa_cache_create.argtypes = [i64, i32, i32, i32, C.POINTER(vp)]
+    lib.gqsa_cache_info.restype = C.c_int
+    lib.gqsa_cache_info.argtypes = [vp, C.POINTER(_CacheInfo)]
+    lib.gqsa_cache_free.restype = None
+    lib.gqsa_cache_free.argtypes = [vp]
+    for name in ("gqsa_cache_append", "gqsa_cache_read"):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = [vp, *heads, *heads, i64, *sequences, vp]
+    lib.gqsa_cache_attend.restype = C.c_int
+    lib.gqsa_cache_attend.argtypes = [vp, *heads, i32, i64, *sequences, C.c_float, *heads, vp]
+    lib.gqsa_prompt_attend.restype = C.c_int
+    lib.gqsa_prompt_attend.argtypes = [*heads, i32, i64, *heads, *heads, i32, i64, i32, vp, vp, i32, C.c_float, *heads, vp]
     lib.gqsa_stream_read_workgroups.restype = C.c_int
     lib.gqsa_stream_read_workgroups.argtypes = []
     _LIB = lib
@@ -428,3 +450,167 @@ def gqsa_stream_read(buf, sink, stream=None) -> None:
     nbytes = buf.numel() * buf.element_size()
     _check(_lib().gqsa_stream_read(C.c_void_p(buf.data_ptr()), nbytes, C.c_void_p(sink.data_ptr()),
                                    _stream_ptr(stream)), "gqsa_stream_read")
+
+
+# ----------------------------------------------------------------------------- between the q/k/v and the o product
+
+def _heads(t, what: str):
+    """(pointer, distance between rows, distance between heads) of a float16 device tensor [rows, heads, head_dim] whose heads are
+    contiguous; the other two dimensions may be strided."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float16:
+        raise ValueError(f"{what} must be a float16 device tensor")
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError(f"{what} must be [rows, heads, head_dim] with contiguous heads")
+    rows, heads, _ = t.shape         # (torch lets the distance of a dimension of size 1 be anything)
+    return t.data_ptr(), t.stride(0) if rows > 1 else 0, t.stride(1) if heads > 1 else 0
+
+
+def _like(x, stream):
+    """A new array of x's shape, for work on `stream` (memory is handed out, and taken back, in the order of a stream's work)."""
+    import torch
+    if stream is None:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    with torch.cuda.stream(stream):
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+
+
+def gqsa_qk_norm_rotate(q, k, positions, table, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                        q_out=None, k_out=None, stream=None):
+    """Norms of queries [rows, q_heads, head_dim] and keys [rows, k_heads, head_dim] per head (weights float16 [head_dim] or None: no norm)
+    and their rotation: positions int32 [rows], table float32 [n_positions, rotary_dim / 2, 2] (cosine, sine), or both None: no
+    rotation.  k None: queries only.  q_out = q, k_out = k: in place.  Returns (q_out, k_out)."""
+    q_at = _heads(q, "q")
+    rows, q_heads, dim = q.shape
+    if q_out is None:
+        q_out = _like(q, stream)
+    if q_out.shape != q.shape:
+        raise ValueError("q_out must have the shape of q")
+    k_heads, k_at, k_out_at = 0, (None, 0, 0), (None, 0, 0)
+    if k is not None:
+        k_at = _heads(k, "k")
+        k_heads = k.shape[1]
+        if k_out is None:
+            k_out = _like(k, stream)
+        if k.shape[0] != rows or k.shape[2] != dim or k_out.shape != k.shape:
+            raise ValueError("k must be [rows, k_heads, head_dim] and k_out as k")
+        k_out_at = _heads(k_out, "k_out")
+    n_positions = rotary = 0
+    if table is not None:
+        if table.dim() != 3 or table.shape[2] != 2 or positions is None or positions.shape != (rows,):
+            raise ValueError("table must be [n_positions, rotary_dim / 2, 2] and positions [rows]")
+        n_positions, rotary = table.shape[0], 2 * table.shape[1]
+    for w in (q_weight, k_weight):
+        if w is not None and w.shape != (dim,):
+            raise ValueError("norm weights must be [head_dim]")
+    _check(_lib().gqsa_qk_norm_rotate(
+        *q_at, q_heads, *k_at, k_heads, rows, dim,
+        None if q_weight is None else _dev_ptr(q_weight, "torch.float16", "q_weight"),
+        None if k_weight is None else _dev_ptr(k_weight, "torch.float16", "k_weight"), eps,
+        _dev_ptr(table, "torch.float32", "table") if rotary else None, n_positions, rotary, int(interleaved),
+        _dev_ptr(positions, "torch.int32", "positions") if rotary else None,
+        *_heads(q_out, "q_out"), *k_out_at, _stream_ptr(stream)), "gqsa_qk_norm_rotate")
+    return q_out, k_out
+
+
+class GqsaCache:
+    """Owns one gqsa_cache_t; freed on gqsa_cache_free() or garbage collection."""
+
+    def __init__(self, ptr: int, kv_heads: int, head_dim: int):
+        self.ptr = C.c_void_p(ptr)
+        self.kv_heads, self.head_dim = kv_heads, head_dim
+
+    def __del__(self):
+        try:
+            gqsa_cache_free(self)
+        except Exception:
+            pass
+
+
+def gqsa_cache_create(n_pages: int, page_tokens: int, kv_heads: int, head_dim: int) -> GqsaCache:
+    out = C.c_void_p()
+    _check(_lib().gqsa_cache_create(n_pages, page_tokens, kv_heads, head_dim, C.byref(out)), "gqsa_cache_create")
+    return GqsaCache(out.value, kv_heads, head_dim)
+
+
+def gqsa_cache_info(c: GqsaCache) -> dict:
+    info = _CacheInfo()
+    _check(_lib().gqsa_cache_info(c.ptr, C.byref(info)), "gqsa_cache_info")
+    return {name: getattr(info, name) for name, _ in _CacheInfo._fields_}
+
+
+def gqsa_cache_free(c: GqsaCache) -> None:
+    """The pages must not be in use any more (as with gqsa_free, work that reads them has to be over)."""
+    if c.ptr is not None and c.ptr.value:
+        _lib().gqsa_cache_free(c.ptr)
+        c.ptr = C.c_void_p()
+
+
+def _sequences(pages, lengths, row_starts):
+    """pages int32 [n_seqs, max_pages], lengths int32 [n_seqs], row_starts int32 [n_seqs + 1] or None (a row per sequence)."""
+    if pages.dim() != 2 or lengths.shape != (pages.shape[0],):
+        raise ValueError("pages must be [n_seqs, max_pages] and lengths [n_seqs]")
+    n = pages.shape[0]
+    starts = None
+    if row_starts is not None:
+        if row_starts.shape != (n + 1,):
+            raise ValueError("row_starts must be [n_seqs + 1]")
+        starts = _dev_ptr(row_starts, "torch.int32", "row_starts")
+    return _dev_ptr(pages, "torch.int32", "pages"), pages.shape[1], _dev_ptr(lengths, "torch.int32", "lengths"), starts, n
+
+
+def _cache_rows(c: GqsaCache, k, v):
+    if k.shape != v.shape or k.dim() != 3 or k.shape[1] != c.kv_heads or k.shape[2] != c.head_dim:
+        raise ValueError("keys and values must be [rows, kv_heads, head_dim] of the cache")
+
+
+def gqsa_cache_append(c: GqsaCache, k, v, pages, lengths, row_starts=None, stream=None) -> None:
+    """New keys and values [rows, kv_heads, head_dim] become the last tokens of their sequences; lengths counts them in."""
+    _cache_rows(c, k, v)
+    _check(_lib().gqsa_cache_append(c.ptr, *_heads(k, "k"), *_heads(v, "v"), k.shape[0], *_sequences(pages, lengths, row_starts),
+                                    _stream_ptr(stream)), "gqsa_cache_append")
+
+
+def gqsa_cache_read(c: GqsaCache, pages, lengths, row_starts, k_out, v_out, stream=None):
+    """The values of the last tokens of each sequence, as many as it has rows in k_out and v_out [rows, kv_heads, head_dim]."""
+    _cache_rows(c, k_out, v_out)
+    _check(_lib().gqsa_cache_read(c.ptr, *_heads(k_out, "k_out"), *_heads(v_out, "v_out"), k_out.shape[0],
+                                  *_sequences(pages, lengths, row_starts), _stream_ptr(stream)), "gqsa_cache_read")
+    return k_out, v_out
+
+
+def gqsa_cache_attend(c: GqsaCache, q, pages, lengths, row_starts=None, scale: float = None, out=None, stream=None):
+    """Attention of the newest rows q [rows, q_heads, head_dim] of each sequence over its cache; scale None: head_dim ** -0.5."""
+    q_at = _heads(q, "q")
+    if q.shape[2] != c.head_dim:
+        raise ValueError("q must be [rows, q_heads, head_dim] of the cache")
+    if out is None:
+        out = _like(q, stream)
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    _check(_lib().gqsa_cache_attend(c.ptr, *q_at, q.shape[1], q.shape[0], *_sequences(pages, lengths, row_starts),
+                                    c.head_dim ** -0.5 if scale is None else scale, *_heads(out, "out"), _stream_ptr(stream)),
+           "gqsa_cache_attend")
+    return out
+
+
+def gqsa_prompt_attend(q, k, v, q_starts, k_starts, scale: float = None, out=None, stream=None):
+    """Causal attention over packed prompts: q [q_rows, q_heads, head_dim], k and v [k_rows, kv_heads, head_dim], starts int32
+    [n_seqs + 1] of each sequence's rows; scale None: head_dim ** -0.5."""
+    q_at, k_at, v_at = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+    dim = q.shape[2]
+    if k.shape != v.shape or k.shape[2] != dim:
+        raise ValueError("k and v must be [k_rows, kv_heads, head_dim]")
+    if q_starts.dim() != 1 or q_starts.shape != k_starts.shape:
+        raise ValueError("q_starts and k_starts must be [n_seqs + 1]")
+    if out is None:
+        out = _like(q, stream)
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    _check(_lib().gqsa_prompt_attend(*q_at, q.shape[1], q.shape[0], *k_at, *v_at, k.shape[1], k.shape[0], dim,
+                                     _dev_ptr(q_starts, "torch.int32", "q_starts"), _dev_ptr(k_starts, "torch.int32", "k_starts"),
+                                     q_starts.shape[0] - 1, dim ** -0.5 if scale is None else scale, *_heads(out, "out"),
+                                     _stream_ptr(stream)), "gqsa_prompt_attend")
+    return out

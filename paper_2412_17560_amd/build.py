@@ -18,7 +18,8 @@ SANITIZED_LIB = os.path.join(OBJ, "libgqsa_host_asan.so")
 # (gqsa_gemv.hip is compiled nine times: whole, once per further tile size and once per pair of the other
 # group sizes -- "file:part")
 SOURCES = ["gqsa_gemv.hip", *(f"gqsa_gemv.hip:{part}" for part in range(1, 9)), "gqsa_pack.cpp", "gqsa_panels.cpp",
-           "gqsa_api.cpp", "gqsa_panel_kernel.hip", "gqsa_pack_device.hip", "gqsa_baselines.hip"]
+           "gqsa_api.cpp", "gqsa_panel_kernel.hip", "gqsa_pack_device.hip", "gqsa_baselines.hip",
+           "gqsa_attention_api.cpp", "gqsa_rotate.hip", "gqsa_cache.hip", "gqsa_prompt.hip"]
 
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
           "-Wall", "-Wextra", "-Wno-unused-parameter"]
@@ -75,7 +76,7 @@ def build_sanitized() -> str:
     side replaced by stubs that answer GQSA_ERR_HIP -- with AddressSanitizer and
     UndefinedBehaviorSanitizer (host code only; no GPU code is compiled or sanitized)."""
     os.makedirs(OBJ, exist_ok=True)
-    srcs = [os.path.join(CSRC, f) for f in ("gqsa_pack.cpp", "gqsa_panels.cpp", "gqsa_api.cpp", "gqsa_host_stubs.cpp")]
+    srcs = [os.path.join(CSRC, f) for f in ("gqsa_pack.cpp", "gqsa_panels.cpp", "gqsa_api.cpp", "gqsa_attention_api.cpp", "gqsa_host_stubs.cpp")]
     cmd = [_hipcc(), "-x", "c++", "-O1", "-g", "-fPIC", "-shared", "-std=c++17", "-fno-gpu-sanitize",
            "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-shared-libsan", "-fno-omit-frame-pointer",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC, *HOST_FLAGS, *srcs, "-o", SANITIZED_LIB, "-lpthread"]

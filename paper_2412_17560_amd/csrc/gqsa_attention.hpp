@@ -1,0 +1,87 @@
+// Internal definitions of the operators between the q/k/v and the o product (include/gqsa_attention.h): what the C boundary
+// (gqsa_attention_api.cpp) hands to the kernels (gqsa_rotate.hip, gqsa_cache.hip, gqsa_prompt.hip).
+#pragma once
+
+#include <cstdint>
+#include <cstdio>
+
+#include "gqsa_attention.h"
+
+// (used where the HIP runtime is included)
+#define GQSA_HIP(call)                                                                   \
+    do {                                                                                 \
+        const hipError_t e_ = (call);                                                    \
+        if (e_ != hipSuccess) {                                                          \
+            std::fprintf(stderr, "libgqsa: %s: %s\n", #call, hipGetErrorString(e_));    \
+            return GQSA_ERR_HIP;                                                         \
+        }                                                                                \
+    } while (0)
+
+namespace gqsa {
+
+// A [rows, heads, head_dim] array of fp16: elements of a head side by side, distances in elements.
+struct Heads {
+    uint16_t* data;
+    int64_t row, head;
+};
+
+struct RotateCall {
+    Heads q, k, q_out, k_out;
+    const uint16_t *q_weight, *k_weight;
+    const float* table;
+    const int32_t* positions;
+    int64_t n_rows, n_positions;
+    int q_heads, k_heads, head_dim, rotary_dim, interleaved;
+    float eps;
+};
+
+// The tokens of a 4-bit cache are held in tiles of 32 of one head: what 16x16x32 products take (gqsa_cache.hip says in which order).
+constexpr int kTileTokens = 32;
+constexpr int kGroupChannels = 32;      // elements that share low and step
+constexpr int tile_bytes(int head_dim) { return kTileTokens * head_dim + 2 * kTileTokens * (head_dim / kGroupChannels) * 4; }
+
+constexpr int kAttendWorkgroups = 1024;     // the most workgroups of one attention over the cache: four to a compute unit
+constexpr int kRowBlock = 16;               // query rows (rows of a sequence times the heads of a group) per product
+
+// Where the rows, pages and lengths of a call's sequences are.
+struct Sequences {
+    const int32_t *pages, *lengths, *row_starts;
+    int64_t n_rows;
+    int max_pages, n_seqs;
+};
+
+}  // namespace gqsa
+
+struct gqsa_cache {
+    int64_t n_pages = 0;
+    int page_tokens = 0, kv_heads = 0, head_dim = 0;
+    int device = -1;
+    uint8_t* d_pages = nullptr;
+    float* d_partials = nullptr;    // kAttendWorkgroups * 2 partial results of up to kRowBlock rows
+    int32_t* d_arrivals = nullptr;  // kAttendWorkgroups counters, zero between calls
+
+    int64_t device_bytes() const { return n_pages * kv_heads * (page_tokens / gqsa::kTileTokens) * int64_t{gqsa::tile_bytes(head_dim)}; }
+    int64_t partial_floats() const { return int64_t{gqsa::kAttendWorkgroups} * 2 * gqsa::kRowBlock * (head_dim + 2); }
+    int64_t workspace_bytes() const { return partial_floats() * 4 + int64_t{gqsa::kAttendWorkgroups} * 4; }
+};
+
+namespace gqsa {
+
+gqsa_status_t rotate(const RotateCall& call, void* stream);
+
+gqsa_status_t cache_allocate(gqsa_cache* c);
+void cache_release(gqsa_cache* c);
+gqsa_status_t cache_append(gqsa_cache* c, const Heads& k, const Heads& v, const Sequences& seqs, void* stream);
+gqsa_status_t cache_read(gqsa_cache* c, const Heads& k, const Heads& v, const Sequences& seqs, void* stream);
+gqsa_status_t cache_attend(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, float scale, const Heads& out, void* stream);
+
+struct PromptCall {
+    Heads q, k, v, out;
+    const int32_t *q_starts, *k_starts;
+    int64_t n_q_rows, n_k_rows;
+    int q_heads, kv_heads, head_dim, n_seqs;
+    float scale;
+};
+gqsa_status_t prompt_attend(const PromptCall& call, void* stream);
+
+}  // namespace gqsa

@@ -3,6 +3,7 @@
 // answers GQSA_ERR_HIP, so that the packer, the image builders and the C boundary can run
 // under AddressSanitizer and UndefinedBehaviorSanitizer on a machine without a GPU.
 // Never linked into libgqsa.so itself.
+#include "gqsa_attention.hpp"
 #include "gqsa_bench.h"
 #include "gqsa_internal.hpp"
 
@@ -17,6 +18,13 @@ bool stream_is_capturing(void*) { return false; }
 gqsa_status_t panels_upload(gqsa_matrix*) { return GQSA_ERR_HIP; }
 void panels_release(gqsa_matrix*) {}
 gqsa_status_t panels_gemm(const gqsa_matrix* const*, int, const void*, void* const*, int, void*) { return GQSA_ERR_HIP; }
+gqsa_status_t rotate(const RotateCall&, void*) { return GQSA_ERR_HIP; }
+gqsa_status_t cache_allocate(gqsa_cache*) { return GQSA_ERR_HIP; }
+void cache_release(gqsa_cache*) {}
+gqsa_status_t cache_append(gqsa_cache*, const Heads&, const Heads&, const Sequences&, void*) { return GQSA_ERR_HIP; }
+gqsa_status_t cache_read(gqsa_cache*, const Heads&, const Heads&, const Sequences&, void*) { return GQSA_ERR_HIP; }
+gqsa_status_t cache_attend(gqsa_cache*, const Heads&, int, const Sequences&, float, const Heads&, void*) { return GQSA_ERR_HIP; }
+gqsa_status_t prompt_attend(const PromptCall&, void*) { return GQSA_ERR_HIP; }
 
 }  // namespace gqsa
 

@@ -1,0 +1,268 @@
+// Causal attention over packed prompts with grouped heads (gqsa_prompt_attend): o = softmax(scale q K^T) V, a row over the keys up to
+// its own.  One pass over the keys with the running maximum and sum of each row; scores never leave the registers.
+//
+// A workgroup of 4 wavefronts takes 128 query rows of one head, a wavefront 32 of them; keys and values come in tiles of 64, copied from
+// memory straight into LDS, one tile ahead of the one at work.  Both products are 32x32x16 ones, taken the other way round --
+// S^T = K Q^T, O^T = V^T P^T -- because then a lane holds scores of one query row only (its maximum and sum need one exchange, between the two
+// halves of the wavefront) and holds them as the second product wants its operand; V^T comes out of LDS by transposing reads.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "gqsa_device.hpp"
+
+namespace gqsa {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlockRows = 128;     // query rows of a workgroup
+constexpr int kWaveRows = 32;
+constexpr int kTileKeys = 64;
+constexpr float kSlack = 8.0f;      // powers of two that a score may lie above its row's reference before the reference follows
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+
+// Where a row of a tile keeps its run `chunk` of 8 elements.  Keys: 16 neighbouring rows read the same run, so the runs are spread by the
+// row over all banks; values: 4 neighbouring rows read 4 neighbouring runs.
+template <int D>
+__device__ __forceinline__ int key_place(int row, int chunk) { return chunk ^ (D == 128 ? row & 15 : (row >> 1) & 7); }
+template <int D>
+__device__ __forceinline__ int value_place(int row, int chunk) { return chunk ^ (D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1)); }
+
+template <int D>
+struct alignas(256) PromptShared {
+    uint16_t k[2][kTileKeys * D], v[2][kTileKeys * D];
+};
+
+__device__ __forceinline__ uint32_t lds_address(const void* p)
+{
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) uint8_t*)p));
+}
+
+// N KiB from memory into LDS at `to`, a KiB at a time: 16 bytes a lane from `from` + at[i].  (The first wait states are for scalar registers
+// that a vector instruction may have written just before, which the compiler does not see to inside a statement; one is for m0.)
+template <int N>
+__device__ __forceinline__ void copy_in(uint32_t to, uint64_t from, const uint32_t (&at)[N])
+{
+    static_assert(N == 2 || N == 4, "");
+    if constexpr (N == 4)
+        asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %2, %1\n\t"
+                     "s_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %1\n\t"
+                     "s_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %1\n\t"
+                     "s_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %1"
+                     : "+{m0}"(to) : "s"(from), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]) : "memory", "scc");
+    else
+        asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %2, %1\n\t"
+                     "s_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %1"
+                     : "+{m0}"(to) : "s"(from), "v"(at[0]), "v"(at[1]) : "memory", "scc");
+}
+
+// Whether the tile of values holds an infinity or a NaN (for the whole wavefront).
+template <int D>
+__device__ __forceinline__ bool any_not_finite(const uint16_t* tile, int lane)
+{
+    uint32_t over = 0;      // the exponent's bits all set: adding its lowest one carries into the sign's place
+#pragma unroll
+    for (int i = 0; i < kTileKeys * D / 512; ++i) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(tile + (i * 64 + lane) * 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) over |= (x[e] & 0x7C007C00u) + 0x04000400u;
+    }
+    return __any((over & 0x80008000u) != 0);
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool negate)
+{
+    constexpr int kCopies = D / 32;                  // KiB of a tile of keys that a wavefront copies
+    constexpr int kCopyRows = 512 / D;               // rows in one of them
+    constexpr int kLanesPerRow = D / 8;
+    __shared__ PromptShared<D> shared;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+
+    const auto rows_of = [](const int32_t* starts, int64_t n, int b, int* start) {
+        const int most = static_cast<int>(n);
+        *start = min(max(starts[b], 0), most);
+        return max(min(starts[b + 1], most) - *start, 0);
+    };
+    const auto blocks_of = [&](int b) {
+        int start;
+        return static_cast<int64_t>((rows_of(c.q_starts, c.n_q_rows, b, &start) + kBlockRows - 1) / kBlockRows);
+    };
+    // Heads vary fastest, those of a group on one XCD (workgroup i runs on XCD i % 8), the last blocks of a sequence -- those with the
+    // most keys -- come first.
+    const int slot = blockIdx.x / c.q_heads, of = blockIdx.x % c.q_heads;
+    const int head = c.q_heads % 8 == 0 ? of % 8 * (c.q_heads / 8) + of / 8 : of;
+    const int64_t total = total_of(c.n_seqs, lane, blocks_of);
+    int b;
+    int64_t block;
+    if (slot >= total || !locate(c.n_seqs, total - 1 - slot, lane, blocks_of, &b, &block)) return;
+    b = __builtin_amdgcn_readfirstlane(b);
+    int q_start, k_start;
+    const int n_q = rows_of(c.q_starts, c.n_q_rows, b, &q_start), n_k = rows_of(c.k_starts, c.n_k_rows, b, &k_start);
+    const int behind = n_k - n_q;                    // row r sees keys 0 .. r + behind
+    const int row0 = __builtin_amdgcn_readfirstlane(static_cast<int>(block)) * kBlockRows, wave_row0 = row0 + wave * kWaveRows;
+    const int row = wave_row0 + (lane & 31);
+    const int sees = row + behind + 1;
+    const int keys = max(min(n_q, row0 + kBlockRows) + behind, 0);                               // that some row of the block sees
+    const int wave_keys = wave_row0 < n_q ? max(min(n_q, wave_row0 + kWaveRows) + behind, 0) : 0;
+    const int tiles = (keys + kTileKeys - 1) / kTileKeys;
+
+    // the query rows, and what this lane copies of a tile
+    half8_t q[D / 16];
+    const uint16_t* q_at = c.q.data + (int64_t{q_start} + min(row, n_q - 1)) * c.q.row + head * c.q.head + 8 * half;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const half8_t*>(q_at + 16 * i);
+    if (negate) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) q[i] = -q[i];
+    }
+    const int kv_head = head / (c.q_heads / c.kv_heads);
+    const uint64_t k_from = reinterpret_cast<uint64_t>(c.k.data + int64_t{k_start} * c.k.row + kv_head * c.k.head);
+    const uint64_t v_from = reinterpret_cast<uint64_t>(c.v.data + int64_t{k_start} * c.v.row + kv_head * c.v.head);
+    const auto copy = [&](int tile, int buffer) {
+        uint32_t k_lane[kCopies], v_lane[kCopies];
+        const int last = n_k - 1 - tile * kTileKeys;      // keys that do not exist are the last one again: no row sees them
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int r = kCopies * kCopyRows * wave + kCopyRows * i + lane / kLanesPerRow, at = lane % kLanesPerRow;
+            k_lane[i] = 2u * (static_cast<uint32_t>(min(r, last)) * static_cast<uint32_t>(c.k.row) + 8u * key_place<D>(r, at));
+            v_lane[i] = 2u * (static_cast<uint32_t>(min(r, last)) * static_cast<uint32_t>(c.v.row) + 8u * value_place<D>(r, at));
+        }
+        const uint32_t to = wave * kCopies * 1024u;
+        copy_in<kCopies>(lds_address(shared.k[buffer]) + to, k_from + uint64_t{2} * (uint64_t{static_cast<uint32_t>(tile * kTileKeys)} * static_cast<uint64_t>(c.k.row)), k_lane);
+        copy_in<kCopies>(lds_address(shared.v[buffer]) + to, v_from + uint64_t{2} * (uint64_t{static_cast<uint32_t>(tile * kTileKeys)} * static_cast<uint64_t>(c.v.row)), v_lane);
+    };
+
+    float16_t out[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) out[i] = float16_t{};
+    float top = kMinusInf, sum = 0.0f;
+
+    if (tiles > 0) copy(0, 0);
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int buffer = tile & 1, first = tile * kTileKeys;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wavefront's part of the tile has arrived,
+        __syncthreads();                                       // everybody's has, and nobody reads the other buffer any more
+        if (tile + 1 < tiles) copy(tile + 1, buffer ^ 1);
+        if (first >= wave_keys) continue;
+
+        const uint16_t* k_tile = shared.k[buffer];
+        float16_t s[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) s[j] = float16_t{};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = 32 * j + (lane & 31);
+                const half8_t k = *reinterpret_cast<const half8_t*>(k_tile + r * D + 8 * key_place<D>(r, 2 * i + half));
+                s[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i], s[j], 0, 0, 0);
+            }
+        }
+        // element r of s[j] is key 32 j + r % 4 + 8 (r / 4) + 4 half
+        const bool edge = first + kTileKeys > wave_row0 + behind + 1;      // some row does not see all of the tile
+        if (edge) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (first + 32 * j + (r & 3) + 8 * (r >> 2) + 4 * half >= sees) s[j][r] = kMinusInf;
+        }
+        float most = kMinusInf;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[j][r]);
+        most *= c.scale;
+        if (__any(most > top + kSlack || (top == kMinusInf && most > kMinusInf))) {
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const float higher = fmaxf(top, most);
+            const float shrink = higher == kMinusInf ? 1.0f : __builtin_amdgcn_exp2f(top - higher);
+            top = higher;
+            sum *= shrink;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) out[i] *= shrink;
+        }
+        const float reference = top == kMinusInf ? 0.0f : top;
+        half8_t p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + e], c.scale, -reference));
+                sum += x;
+                p[i][e] = static_cast<_Float16>(x);
+            }
+        const uint16_t* v_tile = shared.v[buffer];
+        const auto values = [&](int i, int d) {
+            short4_t part[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                // 16 lanes read 4 keys x 16 elements, each 4 elements of a key, and get 4 keys of an element each
+                const int r = 16 * i + 8 * h + 4 * half + ((lane & 15) >> 2), e = 32 * d + (lane & 16) + 4 * (lane & 3);
+                const uint16_t* at = v_tile + r * D + 8 * value_place<D>(r, e >> 3) + (e & 7);
+                part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)at);
+            }
+            return __builtin_shufflevector(__builtin_bit_cast(half4_t, part[0]), __builtin_bit_cast(half4_t, part[1]), 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        if (!edge || !any_not_finite<D>(v_tile, lane)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values(i, d), p[i], out[d], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) {
+                float16_t count = float16_t{};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const half8_t v = values(i, d);
+                    half8_t seen;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) seen[e] = static_cast<_Float16>(first + 16 * i + 8 * (e >> 2) + 4 * half + (e & 3) < sees ? 1.0f : 0.0f);
+                    out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(finite_part(v), p[i], out[d], 0, 0, 0);
+                    count = __builtin_amdgcn_mfma_f32_32x32x16_f16(not_finite(v), seen, count, 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);      // (one after the other: few registers, not speed)
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) out[d][r] += from_counts(count[r]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+
+    sum += __shfl_xor(sum, 32);
+    if (row >= n_q) return;
+    uint16_t* to = c.out.data + (int64_t{q_start} + row) * c.out.row + head * c.out.head + 4 * half;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            half4_t y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = sum == 0.0f ? static_cast<_Float16>(0.0f) : static_cast<_Float16>(out[d][4 * r + e] / sum);
+            *reinterpret_cast<half4_t*>(to + 32 * d + 8 * r) = y;
+        }
+}
+
+}  // namespace
+
+gqsa_status_t prompt_attend(const PromptCall& call, void* stream)
+{
+    PromptCall c = call;
+    const bool negate = c.scale < 0.0f;     // of the queries instead: the largest score is then the one of the largest product
+    // (the softmax is taken to base 2; not 0, so that a masked score stays -infinity: 1e-30 leaves every weight at 1)
+    c.scale = std::max(std::fabs(c.scale) * 1.44269504088896341f, 1e-30f);
+    const int64_t blocks = (c.n_q_rows / kBlockRows + c.n_seqs) * c.q_heads;      // no fewer than there are
+    if (blocks > (int64_t{1} << 23)) return GQSA_ERR_SHAPE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const dim3 grid(static_cast<unsigned>(blocks));
+    if (c.head_dim == 128) hipLaunchKernelGGL(prompt_kernel<128>, grid, dim3(kThreads), 0, s, c, negate);
+    else hipLaunchKernelGGL(prompt_kernel<64>, grid, dim3(kThreads), 0, s, c, negate);
+    GQSA_HIP(hipGetLastError());
+    return GQSA_OK;
+}
+
+}  // namespace gqsa
