@@ -58,18 +58,18 @@ __device__ __forceinline__ void copy_in(uint32_t to, uint64_t from, const uint32
                      : "+{m0}"(to) : "s"(from), "v"(at[0]), "v"(at[1]) : "memory", "scc");
 }
 
-// Whether the tile of values holds an infinity or a NaN (for the whole wavefront).
+// Whether this thread's part of a tile of values holds an infinity or a NaN.
 template <int D>
-__device__ __forceinline__ bool any_not_finite(const uint16_t* tile, int lane)
+__device__ __forceinline__ bool some_not_finite(const uint16_t* tile)
 {
     uint32_t over = 0;      // the exponent's bits all set: adding its lowest one carries into the sign's place
 #pragma unroll
-    for (int i = 0; i < kTileKeys * D / 512; ++i) {
-        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(tile + (i * 64 + lane) * 8);
+    for (int i = 0; i < kTileKeys * D / 8 / kThreads; ++i) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(tile + (i * kThreads + threadIdx.x) * 8);
 #pragma unroll
         for (int e = 0; e < 4; ++e) over |= (x[e] & 0x7C007C00u) + 0x04000400u;
     }
-    return __any((over & 0x80008000u) != 0);
+    return (over & 0x80008000u) != 0;
 }
 
 template <int D>
@@ -146,24 +146,42 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wavefront's part of the tile has arrived,
         __syncthreads();                                       // everybody's has, and nobody reads the other buffer any more
         if (tile + 1 < tiles) copy(tile + 1, buffer ^ 1);
-        if (first >= wave_keys) continue;
+        const bool active = first < wave_keys;                 // (the same for a whole wavefront)
+        const uint16_t *k_tile = shared.k[buffer], *v_tile = shared.v[buffer];
+        // The two (with keys of an earlier part three) tiles that some rows see in part.  If values there are not finite, the rows that do not see them must
+        // be kept from them: see below.
+        bool wild = false;
+        if (first + kTileKeys > row0 + behind + 1) wild = __syncthreads_or(some_not_finite<D>(v_tile));
 
-        const uint16_t* k_tile = shared.k[buffer];
         float16_t s[2];
+        if (active) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) s[j] = float16_t{};
+            for (int j = 0; j < 2; ++j) s[j] = float16_t{};
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
+            for (int i = 0; i < D / 16; ++i) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int r = 32 * j + (lane & 31);
-                const half8_t k = *reinterpret_cast<const half8_t*>(k_tile + r * D + 8 * key_place<D>(r, 2 * i + half));
-                s[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i], s[j], 0, 0, 0);
+                for (int j = 0; j < 2; ++j) {
+                    const int r = 32 * j + (lane & 31);
+                    const half8_t k = *reinterpret_cast<const half8_t*>(k_tile + r * D + 8 * key_place<D>(r, 2 * i + half));
+                    s[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i], s[j], 0, 0, 0);
+                }
             }
         }
+        if (wild) {
+            // the keys have been read: what is not finite moves from the values' tile to the keys', as counts
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kTileKeys * D / 8 / kThreads; ++i) {
+                const int at = (i * kThreads + threadIdx.x) * 8;
+                const half8_t v = *reinterpret_cast<const half8_t*>(&shared.v[buffer][at]);
+                *reinterpret_cast<half8_t*>(&shared.k[buffer][at]) = not_finite(v);
+                *reinterpret_cast<half8_t*>(&shared.v[buffer][at]) = finite_part(v);
+            }
+            __syncthreads();
+        }
+        if (!active) continue;
         // element r of s[j] is key 32 j + r % 4 + 8 (r / 4) + 4 half
-        const bool edge = first + kTileKeys > wave_row0 + behind + 1;      // some row does not see all of the tile
-        if (edge) {
+        if (first + kTileKeys > wave_row0 + behind + 1) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -195,40 +213,35 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
                 sum += x;
                 p[i][e] = static_cast<_Float16>(x);
             }
-        const uint16_t* v_tile = shared.v[buffer];
-        const auto values = [&](int i, int d) {
+        // The operand V^T: 16 lanes read 4 keys x 16 elements, each 4 elements of a key, and get 4 keys of an element each.
+        const auto turned = [&](const uint16_t* tile, int i, int d) {
             short4_t part[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                // 16 lanes read 4 keys x 16 elements, each 4 elements of a key, and get 4 keys of an element each
                 const int r = 16 * i + 8 * h + 4 * half + ((lane & 15) >> 2), e = 32 * d + (lane & 16) + 4 * (lane & 3);
-                const uint16_t* at = v_tile + r * D + 8 * value_place<D>(r, e >> 3) + (e & 7);
+                const uint16_t* at = tile + r * D + 8 * value_place<D>(r, e >> 3) + (e & 7);
                 part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)at);
             }
             return __builtin_shufflevector(__builtin_bit_cast(half4_t, part[0]), __builtin_bit_cast(half4_t, part[1]), 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        if (!edge || !any_not_finite<D>(v_tile, lane)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int d = 0; d < D / 32; ++d) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values(i, d), p[i], out[d], 0, 0, 0);
-        } else {
+            for (int d = 0; d < D / 32; ++d) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(turned(v_tile, i, d), p[i], out[d], 0, 0, 0);
+        if (wild) {
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) {
                 float16_t count = float16_t{};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const half8_t v = values(i, d);
                     half8_t seen;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) seen[e] = static_cast<_Float16>(first + 16 * i + 8 * (e >> 2) + 4 * half + (e & 3) < sees ? 1.0f : 0.0f);
-                    out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(finite_part(v), p[i], out[d], 0, 0, 0);
-                    count = __builtin_amdgcn_mfma_f32_32x32x16_f16(not_finite(v), seen, count, 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);      // (one after the other: few registers, not speed)
+                    count = __builtin_amdgcn_mfma_f32_32x32x16_f16(turned(k_tile, i, d), seen, count, 0, 0, 0);
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) out[d][r] += from_counts(count[r]);
-                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_sched_barrier(0);      // (one after the other: few registers, not speed)
             }
         }
     }
