@@ -51,10 +51,10 @@ gqsa_status_t gqsa_qk_norm_rotate(const void* q, int64_t q_row_stride, int64_t q
  * and in which order, the caller decides and says in every call: pages [device] int32 [n_seqs, max_pages], page
  * pages[b][i] holds the tokens i page_tokens .. of sequence b.
  *
- * 32 elements of one token and head share low = the least of them (fp16, exact) and step = fp16((greatest - low) / 15); codes are
+ * 32 elements of one token and head share low = the least of them (fp16, exact) and step = fp16((greatest - low) / 15), or the next smaller
+ * fp16 number where low + 15 step would otherwise round to infinity; codes are
  * min(15, round-half-even((x - low) / step)), 0 where step is 0, every operation a single fp32 operation.  A code stands for
- * fp16(low + code step), rounded once (an infinity only where a group reaches up to the end of fp16's range).  A group with an infinity
- * or a NaN stands for NaN throughout.
+ * fp16(low + code step), rounded once.  A group with an infinity or a NaN stands for NaN throughout.
  */
 typedef struct gqsa_cache* gqsa_cache_t;
 

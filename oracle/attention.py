@@ -29,6 +29,9 @@ def cache_groups(x):
     g = np.where(bad, np.float32(0), g)
     low = g.min(axis=-1, keepdims=True)
     step = ((g.max(axis=-1, keepdims=True) - low) / np.float32(15)).astype(np.float16)
+    with np.errstate(over="ignore"):
+        beyond = np.isinf((low.astype(np.float64) + 15.0 * step.astype(np.float64)).astype(np.float16))
+    step = np.where(beyond, np.nextafter(step, np.float16(0)), step)
     wide = step.astype(np.float32)
     ratio = np.divide(g - low, wide, out=np.zeros_like(g), where=np.broadcast_to(wide > 0, g.shape))
     codes = np.minimum(np.rint(ratio), np.float32(15)).astype(np.uint8)

@@ -40,7 +40,7 @@ constexpr int kTileTokens = 32;
 constexpr int kGroupChannels = 32;      // elements that share low and step
 constexpr int tile_bytes(int head_dim) { return kTileTokens * head_dim + 2 * kTileTokens * (head_dim / kGroupChannels) * 4; }
 
-constexpr int kAttendWorkgroups = 1024;     // the most workgroups of one attention over the cache: four to a compute unit
+constexpr int kAttendWorkgroups = 512;      // the most workgroups of one attention over the cache: two to a compute unit
 constexpr int kRowBlock = 16;               // query rows (rows of a sequence times the heads of a group) per product
 
 // Where the rows, pages and lengths of a call's sequences are.
@@ -57,12 +57,12 @@ struct gqsa_cache {
     int page_tokens = 0, kv_heads = 0, head_dim = 0;
     int device = -1;
     uint8_t* d_pages = nullptr;
-    float* d_partials = nullptr;    // kAttendWorkgroups * 2 partial results of up to kRowBlock rows
-    int32_t* d_arrivals = nullptr;  // kAttendWorkgroups counters, zero between calls
+    float* d_partials = nullptr;    // partial results of up to kRowBlock rows: two of every workgroup, one of several together
+    int32_t* d_arrivals = nullptr;  // two counters for every workgroup, zero between calls
 
     int64_t device_bytes() const { return n_pages * kv_heads * (page_tokens / gqsa::kTileTokens) * int64_t{gqsa::tile_bytes(head_dim)}; }
-    int64_t partial_floats() const { return int64_t{gqsa::kAttendWorkgroups} * 2 * gqsa::kRowBlock * (head_dim + 2); }
-    int64_t workspace_bytes() const { return partial_floats() * 4 + int64_t{gqsa::kAttendWorkgroups} * 4; }
+    int64_t partial_floats() const { return int64_t{gqsa::kAttendWorkgroups} * 3 * gqsa::kRowBlock * (head_dim + 2); }
+    int64_t workspace_bytes() const { return partial_floats() * 4 + int64_t{gqsa::kAttendWorkgroups} * 2 * 4; }
 };
 
 namespace gqsa {

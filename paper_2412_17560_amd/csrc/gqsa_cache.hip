@@ -8,11 +8,12 @@
 //            (words w of all lanes: byte (w / 4) 1024 + l 16 + (w % 4) 4 of the region)
 //   key parameters    token by token, group by group: low, step;
 //   value parameters  group by group, quad by quad: step of those 8 tokens, low of those 8 tokens.
-// Code e of a word is at bits 4 (e / 2) + 16 (e % 2), so that one AND leaves two neighbouring ones in the halves of a register.
+// Code e of a word is at bits 8 (e % 4) + 4 (e / 4), so that one AND leaves four neighbouring ones in the bytes of a register.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <climits>
+#include <cmath>
 
 #include "gqsa_device.hpp"
 
@@ -20,10 +21,9 @@ namespace gqsa {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 
 __host__ __device__ constexpr int word_offset(int w, int lane) { return (w >> 2) * 1024 + lane * 16 + (w & 3) * 4; }
-__host__ __device__ constexpr int nibble(int e) { return 4 * (e >> 1) + 16 * (e & 1); }
+__host__ __device__ constexpr int nibble(int e) { return 8 * (e & 3) + 4 * (e >> 2); }
 // The token of slot i of a word of value codes, and back.
 __host__ __device__ constexpr int slot_token(int quad, int i) { return 4 * quad + (i & 3) + (i & 4) * 4; }
 
@@ -64,7 +64,7 @@ struct CopyArgs {
 };
 
 // The tiles that the rows of a sequence lie in, from the first one's (which may be below 0) on.
-__device__ __forceinline__ int64_t tiles_of_rows(const Sequence& q)
+__device__ __forceinline__ int tiles_of_rows(const Sequence& q)
 {
     return q.rows == 0 ? 0 : ((q.length - 1) >> 5) - ((q.length - q.rows) >> 5) + 1;
 }
@@ -77,12 +77,12 @@ struct Unit {
 
 __device__ __forceinline__ bool unit_of(const CopyArgs& a, Unit* u)
 {
-    int b;
-    int64_t within;
-    const auto count = [&](int s) { return tiles_of_rows(sequence(a.seqs, a.pool.page_shift, s)); };
-    if (!locate(a.seqs.n_seqs, blockIdx.x, threadIdx.x & 63, count, &b, &within)) return false;
+    const Deal deal(a.seqs.n_seqs, threadIdx.x & 63, [&](int s) { return static_cast<unsigned>(tiles_of_rows(sequence(a.seqs, a.pool.page_shift, s))); });
+    if (blockIdx.x >= deal.total) return false;
+    int b, within;
+    deal.locate(blockIdx.x, &b, &within);
     u->seq = sequence(a.seqs, a.pool.page_shift, b);
-    u->tile = ((u->seq.length - u->seq.rows) >> 5) + static_cast<int>(within);
+    u->tile = ((u->seq.length - u->seq.rows) >> 5) + within;
     u->head = blockIdx.y;
     u->page = -1;
     if (u->tile >= 0) {
@@ -117,7 +117,9 @@ __device__ __forceinline__ Quantised<N> quantise(const half8_t (&x)[N / 8])
     }
     Quantised<N> q;
     q.low = bad ? static_cast<_Float16>(__builtin_nanf("")) : static_cast<_Float16>(low);
-    q.step = bad ? static_cast<_Float16>(0.0f) : static_cast<_Float16>((high - low) / 15.0f);
+    uint16_t step_bits = __builtin_bit_cast(uint16_t, static_cast<_Float16>(bad ? 0.0f : (high - low) / 15.0f));
+    if (low + 15.0f * static_cast<float>(__builtin_bit_cast(_Float16, step_bits)) >= 65520.0f) --step_bits;       // (what rounds to infinity)
+    q.step = __builtin_bit_cast(_Float16, step_bits);
     const float step = static_cast<float>(q.step);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -241,28 +243,29 @@ struct AttendArgs {
     float* partials;
     int32_t* arrivals;
     int heads_per_group;
-    float scale_log2;       // scale times log2(e): the softmax is taken to base 2
+    float scale_log2;       // |scale| times log2(e): the softmax is taken to base 2
+    bool negate;            // the queries, as scale is negative: the largest score is then the one of the largest product
 };
 
 // A tile as it is loaded: codes of keys and of values, parameters (16 bytes a lane with D = 128, 8 with D = 64).
 template <int D>
 struct Raw {
+    typedef uint32_t words_t __attribute__((ext_vector_type(D / 32)));
     u32x4_t k[D / 64], v[D / 64];
-    uint32_t parameters[D / 32];
+    words_t parameters;
+    int first_token;        // -1: no tile
 };
 
-// Two fp16 numbers of eight codes each time: (x & mask) in the low bits of 1024 (0x6400), taken off again, is exact, and so is
-// the multiply-add by 1/16 for codes four bits higher up.
+// Eight codes as four pairs of fp16 numbers.  A byte 0000cccc is the fp8 (E4M3) number c 2^-9 -- subnormal up to 7, of the lowest exponent from 8 on -- so
+// that the conversion from fp8 with a scale of 2^9 gives c, exactly, two at a time: seven instructions (with the code spliced into the low bits of
+// 1024, which is then taken off, nine, three of them dearer).
 __device__ __forceinline__ void decode(uint32_t x, half2_t (&q)[4])
 {
-    const half2_t off = {static_cast<_Float16>(-1024.0f), static_cast<_Float16>(-1024.0f)};
-    const half2_t sixteenth = {static_cast<_Float16>(0.0625f), static_cast<_Float16>(0.0625f)};
-    const half2_t off16 = {static_cast<_Float16>(-64.0f), static_cast<_Float16>(-64.0f)};
-    const uint32_t y = x >> 8;
-    q[0] = __builtin_bit_cast(half2_t, (x & 0x000F000Fu) | 0x64006400u) + off;
-    q[1] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (x & 0x00F000F0u) | 0x64006400u), sixteenth, off16);
-    q[2] = __builtin_bit_cast(half2_t, (y & 0x000F000Fu) | 0x64006400u) + off;
-    q[3] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (y & 0x00F000F0u) | 0x64006400u), sixteenth, off16);
+    const uint32_t even = x & 0x0F0F0F0Fu, odd = x >> 4 & 0x0F0F0F0Fu;
+    q[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(even, 512.0f, false);
+    q[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(even, 512.0f, true);
+    q[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(odd, 512.0f, false);
+    q[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(odd, 512.0f, true);
 }
 
 __device__ __forceinline__ half8_t join(half2_t a, half2_t b, half2_t c, half2_t d)
@@ -292,42 +295,80 @@ struct RowState {
 
 constexpr float kSlack = 8.0f;      // powers of two that a score may lie above the reference before the reference follows
 
-// One tile for one wavefront.  S^T = K Q^T and O^T = V^T P^T: a lane's scores are then the elements of the operand P^T that the second product wants
-// from it, whatever the tokens' order, as the value codes lie in the same.
+// Of a lane's words of a tile's parameters, clears those of the tokens from `left` on, so that they stand for zero.
 template <int D>
-__device__ __forceinline__ void attend_tile(const Raw<D>& raw, uint32_t* stage, const half8_t (&q)[D / 32], RowState<D>& state, int lane,
-                                            int first_token, int length, int limit, bool edge, float scale_log2)
+__device__ __forceinline__ void hide(typename Raw<D>::words_t& parameters, int lane, int left)
 {
-    constexpr int kWords = D / 32;            // words of parameters a lane stages
-    const int quad = lane >> 4;
-    uint32_t parameters[kWords];
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) parameters[i] = raw.parameters[i];
-    if (edge) {
-        // whatever lies behind the last token (older codes, NaN) stands for zero
-        const int left = length - first_token;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            const int at = (lane * kWords + i) * 4;
-            if (at < 4 * D) {
-                if (at / (D / 8) >= left) parameters[i] = 0;
-            } else {
-                const int o = at - 4 * D, t = slot_token((o >> 5) & 3, (o & 15) >> 1);
-                if (t >= left) parameters[i] = 0;
-                else if (t + 1 >= left) parameters[i] &= 0xFFFFu;
-            }
+    for (int i = 0; i < D / 32; ++i) {
+        const int at = (lane * (D / 32) + i) * 4;
+        if (at < 4 * D) {
+            if (at / (D / 8) >= left) parameters[i] = 0;
+        } else {
+            const int o = at - 4 * D, t = slot_token((o >> 5) & 3, (o & 15) >> 1);
+            if (t >= left) parameters[i] = 0;
+            else if (t + 1 >= left) parameters[i] &= 0xFFFFu;
         }
     }
+}
+
+// The same number, of which the compiler does not know that: what is computed from it stays where it is written, in a branch that is seldom taken,
+// rather than ahead of the loop in registers that are not there.
+__device__ __forceinline__ int opaque(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// One tile for one wavefront.  S^T = K Q^T and O^T = V^T P^T: a lane's scores are then the elements of the operand P^T that the second product wants
+// from it, whatever the tokens' order, as the value codes lie in the same.
+template <int D, bool EDGE>
+__device__ __forceinline__ void attend_tile(const Raw<D>& raw, uint32_t* stage, const half8_t (&q)[D / 32], RowState<D>& state, int lane,
+                                            int length, int limit, float scale_log2)
+{
+    const int first_token = raw.first_token;
+    typedef typename Raw<D>::words_t words_t;
+    const int quad = lane >> 4;
+    words_t parameters = raw.parameters;
+    if constexpr (EDGE) hide<D>(parameters, opaque(lane), length - first_token);      // (older codes, NaN)
     wave_lds_order();
+    reinterpret_cast<words_t*>(stage)[lane] = parameters;
+    wave_lds_order();
+    // Where rows differ in what they see of the tile, a value that is NaN (others are finite) would reach the rows that do not see it.  Such
+    // groups of values stand for zero in the products; which tokens they are of, nan_of says.
+    uint32_t nan_of[D / 32];
+    bool wild = false;
+    if constexpr (EDGE) {
+        bool odd = false;
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) stage[lane * kWords + i] = parameters[i];
-    wave_lds_order();
+        for (int i = 0; i < D / 32; ++i) odd |= ((parameters[i] & 0x7C007C00u) + 0x04000400u & 0x80008000u) != 0;
+        wild = __any(odd);
+        if (wild) {
+            const int t = opaque(lane) & 31, slot = (t & 3) + (t >> 4) * 4;
+#pragma unroll
+            for (int g = 0; g < D / 32; ++g) {
+                const half2_t low = as_half2(stage[D + (g * 4 + (t >> 2 & 3)) * 8 + 4 + (slot >> 1)]);
+                const _Float16 v = low[slot & 1];
+                nan_of[g] = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(v != v));
+            }
+            if (opaque(lane) >= 32) {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const half2_t h = as_half2(parameters[i]);
+                    parameters[i] &= (h[0] == h[0] ? 0xFFFFu : 0u) | (h[1] == h[1] ? 0xFFFF0000u : 0u);
+                }
+            }
+            wave_lds_order();
+            reinterpret_cast<words_t*>(stage)[lane] = parameters;
+            wave_lds_order();
+        }
+    }
 
     float4_t s[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         s[j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        const uint32_t* p = stage + (16 * j + (lane & 15)) * (D / 32);
+        const words_t p = *reinterpret_cast<const words_t*>(stage + (16 * j + (lane & 15)) * (D / 32));
 #pragma unroll
         for (int g = 0; g < D / 32; ++g) {
             const int w = j * (D / 32) + g;
@@ -340,15 +381,30 @@ __device__ __forceinline__ void attend_tile(const Raw<D>& raw, uint32_t* stage, 
             s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(c[0], c[1], c[2], c[3]), q[g], s[j], 0, 0, 0);
         }
     }
-    float x[8];
+    half8_t value[D / 16];         // (ahead of the softmax, whose chain of waits this fills)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3] * scale_log2;
-    if (edge) {
+    for (int g = 0; g < D / 32; ++g) {
+        const u32x4_t* at = reinterpret_cast<const u32x4_t*>(stage + D + (g * 4 + quad) * 8);
+        const u32x4_t step = at[0], low = at[1];               // of the quad's tokens
+#pragma unroll
+        for (int c = 2 * g; c < 2 * g + 2; ++c) {
+            half2_t v[4];
+            decode(raw.v[c >> 2][c & 3], v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __builtin_elementwise_fma(v[i], as_half2(step[i]), as_half2(low[i]));
+            value[c] = join(v[0], v[1], v[2], v[3]);
+        }
+    }
+    if constexpr (EDGE) {
+        const int left = limit - first_token - 4 * opaque(quad);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (first_token + slot_token(quad, i) >= limit) x[i] = kMinusInf;
+            if (slot_token(0, i) >= left) s[i >> 2][i & 3] = kMinusInf;
     }
-    float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    float most = kMinusInf;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = fmaxf(most, s[i >> 2][i & 3]);
+    most *= scale_log2;
     // The reference follows only where a score lies far above it: p then reaches 2^8 at most, well inside fp16.
     if (__any(most > state.top + kSlack || (state.top == kMinusInf && most > kMinusInf))) {
         most = fmaxf(most, __shfl_xor(most, 16));
@@ -363,56 +419,29 @@ __device__ __forceinline__ void attend_tile(const Raw<D>& raw, uint32_t* stage, 
     const float reference = state.top == kMinusInf ? 0.0f : state.top;
     half8_t p;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float e = __builtin_amdgcn_exp2f(x[i] - reference);
-        state.sum += e;
-        p[i] = static_cast<_Float16>(e);
-    }
-    const auto values = [&](int c) {
-        const uint32_t* at = stage + D + (c / 2 * 4 + quad) * 8;
-        half2_t v[4];
-        decode(raw.v[c >> 2][c & 3], v);
+    for (int i = 0; i < 8; ++i) p[i] = static_cast<_Float16>(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][i & 3], scale_log2, -reference)));
+    // (the sum of the weights as the product has them, rounded: half the additions)
+    const half2_t ones = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __builtin_elementwise_fma(v[i], as_half2(at[i]), as_half2(at[4 + i]));
-        return join(v[0], v[1], v[2], v[3]);
-    };
-    // Only where rows differ in what they see of the tile can a value that is not finite reach a row that does not see it.
-    bool wild = false;
-    if (edge) {
-        bool odd = false;
+    for (int i = 0; i < 4; ++i) state.sum = __builtin_amdgcn_fdot2(half2_t{p[2 * i], p[2 * i + 1]}, ones, state.sum, false);
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            const half2_t h = as_half2(parameters[i]);
-            odd |= !(__builtin_fabsf16(h[0]) <= static_cast<_Float16>(65504.0f)) || !(__builtin_fabsf16(h[1]) <= static_cast<_Float16>(65504.0f));
-        }
-        wild = __any(odd);
-    }
-    if (!wild) {
+    for (int c = 0; c < D / 16; ++c) state.out[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value[c], p, state.out[c], 0, 0, 0);
+    if (EDGE && wild) {
+        const int left = limit - first_token;
+        const uint32_t sees = left >= 32 ? ~0u : (1u << max(left, 0)) - 1u;
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) state.out[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values(c), p, state.out[c], 0, 0, 0);
-    } else {
-        half8_t sees;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sees[i] = static_cast<_Float16>(first_token + slot_token(quad, i) < limit ? 1.0f : 0.0f);
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-            const half8_t v = values(c);
-            state.out[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(finite_part(v), p, state.out[c], 0, 0, 0);
-            const float4_t count = __builtin_amdgcn_mfma_f32_16x16x32_f16(not_finite(v), sees, float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) state.out[c][r] += from_counts(count[r]);
-            __builtin_amdgcn_sched_barrier(0);      // (one after the other: few registers, not speed)
-        }
+        for (int g = 0; g < D / 32; ++g)
+            if (nan_of[g] & sees) state.out[2 * g] = state.out[2 * g + 1] = __builtin_nanf("") + float4_t{};
     }
 }
 
 __device__ __forceinline__ float weight_of(float top, float most) { return top == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(top - most); }
 
-template <int D>
+template <int D, int WAVES>
 struct alignas(16) AttendShared {
-    uint32_t stage[kWaves][2 * D];
-    float out[kWaves][kRowBlock][D + 4];       // (+ 4: rows start in different banks)
-    float top[kWaves][kRowBlock], sum[kWaves][kRowBlock];
+    uint32_t stage[WAVES][2 * D];
+    float out[WAVES][kRowBlock][D + 4];       // (+ 4: rows start in different banks)
+    float top[WAVES][kRowBlock], sum[WAVES][kRowBlock];
     int last;
 };
 
@@ -428,66 +457,127 @@ __device__ __forceinline__ float2 load_partial(const float* at)
     return {__builtin_bit_cast(float, static_cast<uint32_t>(both)), __builtin_bit_cast(float, static_cast<uint32_t>(both >> 32))};
 }
 
-constexpr int kStepTiles = kWaves;      // a step: one tile for every wavefront of a workgroup
+constexpr int kHeld = 2;             // tiles that a wavefront holds: the one at work, and those under way
+constexpr int kAttendWaves = 4;      // wavefronts of a workgroup; a step: one tile for each
 
-// The work is dealt by steps of 128 tokens, not by sequences or heads: workgroup w takes the steps w T / W .. (w + 1) T / W - 1 of all T, in the order
-// sequence, head, block of 16 rows, token.  Where a segment (one block of rows of one head) lies in several workgroups, each leaves its maximum,
-// sum and weighted sum in the workspace, and the last to arrive joins them in the order of the tokens.
-template <int D>
-__global__ __launch_bounds__(kThreads, 4) void attend_kernel(AttendArgs a)
+// Joins `parts` partial results of `rows` rows in their order -- part_of(p): maximum, sum, weighted sum -- and hands each four elements of a row to `sink`.  With few rows
+// teams of threads take every so manieth part and meet in `scratch` (LDS).  Called by a whole workgroup.
+template <int D, int THREADS, typename PartOf, typename Sink>
+__device__ __forceinline__ void join(int rows, int parts, float* scratch, PartOf part_of, Sink sink)
 {
+    constexpr int kAhead = 4;       // parts whose loads are under way together
+    const int columns = rows * (D / 4), teams = max(1, THREADS / columns);
+    for (int i = threadIdx.x; i < columns * teams; i += THREADS) {
+        const int team = teams == 1 ? 0 : i / columns, of = i - team * columns, r = of / (D / 4), column = 4 * (of % (D / 4));
+        float top = kMinusInf, s = 0.0f;
+        float4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int p0 = team; p0 < parts; p0 += teams * kAhead) {
+            float2 x[kAhead], y[kAhead], z[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const float* part = part_of(min(p0 + j * teams, parts - 1));
+                x[j] = load_partial(part + r * D + column);
+                y[j] = load_partial(part + r * D + column + 2);
+                z[j] = load_partial(part + kRowBlock * D + 2 * r);
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                if (p0 + j * teams >= parts) break;
+                const float both = fmaxf(top, z[j].x);
+                const float f = weight_of(top, both), g = weight_of(z[j].x, both);
+                s = f * s + g * z[j].y;
+                v = f * v + g * float4_t{x[j].x, x[j].y, y[j].x, y[j].y};
+                top = both;
+            }
+        }
+        if (teams == 1) {
+            sink(r, column, v, top, s);
+        } else {
+            float* at = scratch + i * 6;
+            at[0] = top, at[1] = s, at[2] = v[0], at[3] = v[1], at[4] = v[2], at[5] = v[3];
+        }
+    }
+    if (teams == 1) return;
+    __syncthreads();
+    for (int of = threadIdx.x; of < columns; of += THREADS) {
+        float top = kMinusInf;
+        for (int k = 0; k < teams; ++k) top = fmaxf(top, scratch[(k * columns + of) * 6]);
+        float s = 0.0f;
+        float4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < teams; ++k) {
+            const float* p = scratch + (k * columns + of) * 6;
+            const float f = weight_of(p[0], top);
+            s += f * p[1];
+            v += f * float4_t{p[2], p[3], p[4], p[5]};
+        }
+        sink(of / (D / 4), 4 * (of % (D / 4)), v, top, s);
+    }
+    __syncthreads();       // (`scratch` is free again)
+}
+
+constexpr int kFan = 16;        // parts that one workgroup joins alone
+
+// The work is dealt by steps of 128 tokens, not by sequences or heads: of all steps, in the order sequence, head, block of 16 rows, token, every
+// workgroup takes a run, all of one length or one more.  Where a segment (one block of rows of one head) lies in several workgroups, each
+// leaves its maximum, sum and weighted sum in the workspace, and the last to arrive joins them in the order of the tokens.
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
+{
+    constexpr int kThreads = 64 * WAVES, kStepTiles = WAVES;
     constexpr int kPartial = kRowBlock * (D + 2);
-    __shared__ AttendShared<D> shared;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
-    const int per = a.heads_per_group;
-    const auto blocks_of = [&](const Sequence& q) { return (int64_t{q.rows} * per + kRowBlock - 1) / kRowBlock; };
-    const auto steps_of = [&](const Sequence& q) { return max((q.length + kStepTiles * kTileTokens - 1) / (kStepTiles * kTileTokens), 1); };
-    const auto count = [&](int b) {
+    __shared__ AttendShared<D, WAVES> shared;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), quad = lane >> 4;
+    const unsigned per = a.heads_per_group;
+    const auto blocks_of = [&](const Sequence& q) { return static_cast<int>((static_cast<unsigned>(q.rows) * per + kRowBlock - 1) / kRowBlock); };
+    const auto steps_of = [](const Sequence& q) { return max((q.length + kStepTiles * kTileTokens - 1) / (kStepTiles * kTileTokens), 1); };
+    const Deal deal(a.seqs.n_seqs, lane, [&](int b) {
         const Sequence q = sequence(a.seqs, a.pool.page_shift, b);
-        return blocks_of(q) * steps_of(q) * a.pool.kv_heads;
-    };
-    const int64_t total = total_of(a.seqs.n_seqs, lane, count);
-    const int64_t workers = min(static_cast<int64_t>(gridDim.x), total);
-    const int64_t me = blockIdx.x;
+        return static_cast<unsigned>(min(static_cast<int64_t>(blocks_of(q)) * steps_of(q) * a.pool.kv_heads, int64_t{INT_MAX}));
+    });
+    const unsigned total = deal.total, workers = min(gridDim.x, total), me = blockIdx.x;
     if (me >= workers) return;
-    int64_t at = me * total / workers;
-    const int64_t end = (me + 1) * total / workers;
-    int b;
-    int64_t within;
-    if (!locate(a.seqs.n_seqs, at, lane, count, &b, &within)) return;
-    b = __builtin_amdgcn_readfirstlane(b);
+    const unsigned share = total / workers, more = total - share * workers;      // the first `more` workgroups take one step more
+    const auto start_of = [&](unsigned w) { return w * share + min(w, more); };
+    const auto owner_of = [&](unsigned step) {
+        const unsigned longer = more * (share + 1);
+        return step < longer ? step / (share + 1) : more + (step - longer) / share;
+    };
+    int at = start_of(me);
+    const int end = start_of(me + 1);
+    int b, within;
+    deal.locate(at, &b, &within);
 
     Sequence seq = sequence(a.seqs, a.pool.page_shift, b);
     while (at < end) {
-        const int64_t blocks = blocks_of(seq);
-        const int steps = steps_of(seq);
+        const int blocks = blocks_of(seq), steps = steps_of(seq);
         if (within >= blocks * steps * a.pool.kv_heads) {       // (on to the next sequence that has rows)
             within = 0;
             seq = sequence(a.seqs, a.pool.page_shift, ++b);
             continue;
         }
-        const int64_t segment = within / steps;
-        const int from = static_cast<int>(within - segment * steps);
-        const int to = static_cast<int>(min(static_cast<int64_t>(steps), from + (end - at)));
-        const int head = static_cast<int>(segment / blocks);
-        const int64_t row0 = (segment - head * blocks) * kRowBlock;        // of the sequence's rows times the heads of a group
-        const int rows = static_cast<int>(min(int64_t{kRowBlock}, int64_t{seq.rows} * per - row0));
+        const int segment = static_cast<unsigned>(within) / static_cast<unsigned>(steps), from = within - segment * steps;
+        const int to = min(steps, from + (end - at));
+        const int head = blocks == 1 ? segment : static_cast<unsigned>(segment) / static_cast<unsigned>(blocks);
+        const unsigned row0 = (segment - head * blocks) * kRowBlock;        // of the sequence's rows times the heads of a group
+        const int rows = min(static_cast<unsigned>(kRowBlock), seq.rows * per - row0);
+        const unsigned token0 = row0 / per, head0 = row0 - token0 * per;    // row r of the block: head (head0 + r) % per of the group, token further on
+        const int before = seq.length - seq.rows;
 
         // this lane's row
-        const int64_t mine = row0 + (lane & 15);
         const bool is_row = (lane & 15) < rows;
-        const int row = is_row ? static_cast<int>(mine / per) : 0;
-        const int q_head = head * per + static_cast<int>(mine - int64_t{row} * per);
-        const int limit = is_row ? seq.length - seq.rows + row + 1 : 0;     // tokens it sees
+        const unsigned ahead = (head0 + (lane & 15)) / per;
+        const int row = token0 + ahead, q_head = head * per + (head0 + (lane & 15) - ahead * per);
+        const int limit = is_row ? before + row + 1 : 0;     // tokens it sees
         half8_t q[D / 32];
+        const uint16_t* q_at = a.q.data + int64_t{seq.start + row} * a.q.row + q_head * a.q.head + 8 * quad;
 #pragma unroll
         for (int g = 0; g < D / 32; ++g) {
             q[g] = half8_t{};
-            if (is_row) q[g] = *reinterpret_cast<const half8_t*>(a.q.data + (int64_t{seq.start} + row) * a.q.row + q_head * a.q.head + 32 * g + 8 * quad);
+            if (is_row) q[g] = *reinterpret_cast<const half8_t*>(q_at + 32 * g);
+            if (a.negate) q[g] = -q[g];
         }
-        const int least = seq.length - seq.rows + static_cast<int>(row0 / per) + 1;                 // tokens that the block's first and last row see
-        const int most = seq.length - seq.rows + static_cast<int>((row0 + rows - 1) / per) + 1;
-        const int tiles = min((max(most, 0) + kTileTokens - 1) / kTileTokens, to * kStepTiles);
+        const int least = before + token0 + 1, most = before + token0 + (head0 + rows - 1) / per + 1;    // tokens that the block's first and last row see
+        const int tiles = uniform(min((max(most, 0) + kTileTokens - 1) / kTileTokens, to * kStepTiles));
 
         RowState<D> state;
         state.top = kMinusInf;
@@ -495,33 +585,44 @@ __global__ __launch_bounds__(kThreads, 4) void attend_kernel(AttendArgs a)
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) state.out[c] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
+        // The wavefront's tiles are every kStepTiles-th one; lane i knows the page of the i-th of the next 64, so that no load waits for another.
         const int32_t* table = a.seqs.pages + int64_t{b} * a.seqs.max_pages;
-        const auto load = [&](int t, Raw<D>& raw) {
-            const int page = __builtin_amdgcn_readfirstlane(table[t >> (a.pool.page_shift - 5)]);
-            if (page < 0 || page >= a.pool.n_pages) return false;
-            const uint8_t* tile = a.pool.tile<D>(page, head, t);
+        const int first_tile = uniform(from * kStepTiles + wave), count = max(tiles - first_tile + kStepTiles - 1, 0) / kStepTiles;
+        int page_of_lane = 0;
+        // (always the same number of loads, past the end and for absent pages of some tile that is there: where loads are sometimes left out, the
+        // compiler cannot tell those of the tile at work from those under way, and waits for all)
+        const auto load = [&](int i, Raw<D>& raw) {
+            const int of = min(i, count - 1);
+            if ((i & 63) == 0 && i < count) page_of_lane = opaque(table[min(first_tile + (i + lane) * kStepTiles, tiles - 1) >> (a.pool.page_shift - 5)]);
+            const int page = __builtin_amdgcn_readlane(page_of_lane, of & 63);
+            const bool there = page >= 0 && page < a.pool.n_pages;
+            const int t = first_tile + of * kStepTiles;
+            raw.first_token = there && i < count ? t * kTileTokens : -1;
+            const uint8_t* tile = a.pool.tile<D>(there ? page : 0, head, t);
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) {
-                raw.k[i] = *reinterpret_cast<const u32x4_t*>(tile + i * 1024 + lane * 16);
-                raw.v[i] = *reinterpret_cast<const u32x4_t*>(tile + 16 * D + i * 1024 + lane * 16);
+            for (int w = 0; w < D / 64; ++w) {
+                raw.k[w] = *reinterpret_cast<const u32x4_t*>(tile + w * 1024 + lane * 16);
+                raw.v[w] = *reinterpret_cast<const u32x4_t*>(tile + 16 * D + w * 1024 + lane * 16);
             }
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(tile + 32 * D) + lane * (D / 32);
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) raw.parameters[i] = p[i];
-            return true;
+            raw.parameters = *reinterpret_cast<const typename Raw<D>::words_t*>(tile + 32 * D + lane * (D / 8));
         };
-        Raw<D> next;
-        bool there = false;
-        int t = from * kStepTiles + wave;
-        if (t < tiles) there = load(t, next);
-        while (t < tiles) {
-            const Raw<D> raw = next;
-            const bool here = there;
-            const int now = t;
-            t += kStepTiles;
-            if (t < tiles) there = load(t, next);
-            const int first_token = now * kTileTokens;
-            if (here) attend_tile<D>(raw, shared.stage[wave], q, state, lane, first_token, seq.length, limit, first_token + kTileTokens > least, a.scale_log2);
+        const auto attend = [&](const Raw<D>& raw) {
+            if (raw.first_token < 0) return;
+            if (raw.first_token + kTileTokens > least) attend_tile<D, true>(raw, shared.stage[wave], q, state, lane, seq.length, limit, a.scale_log2);
+            else attend_tile<D, false>(raw, shared.stage[wave], q, state, lane, seq.length, limit, a.scale_log2);
+        };
+        // kHeld - 1 tiles ahead, in registers that are not copied
+        if (count > 0) {
+            Raw<D> held[kHeld];
+#pragma unroll
+            for (int i = 0; i < kHeld - 1; ++i) load(i, held[i]);
+            for (int i = 0; i < count; i += kHeld) {
+#pragma unroll
+                for (int j = 0; j < kHeld; ++j) {
+                    load(i + j + kHeld - 1, held[(j + kHeld - 1) % kHeld]);
+                    attend(held[j]);
+                }
+            }
         }
 
         // the wavefronts' results together
@@ -535,98 +636,65 @@ __global__ __launch_bounds__(kThreads, 4) void attend_kernel(AttendArgs a)
         __syncthreads();
         const bool whole = from == 0 && to == steps;
         const auto write = [&](int r, int column, float4_t v, float s) {
-            const int64_t of = row0 + r;
-            const int token = static_cast<int>(of / per);
-            const int to_head = head * per + static_cast<int>(of - int64_t{token} * per);
+            const unsigned on = (head0 + r) / per;
+            const int to_head = head * per + (head0 + r - on * per);
             half4_t y;
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[i] = s == 0.0f ? static_cast<_Float16>(0.0f) : static_cast<_Float16>(v[i] / s);
-            *reinterpret_cast<half4_t*>(a.out.data + (int64_t{seq.start} + token) * a.out.row + to_head * a.out.head + column) = y;
+            *reinterpret_cast<half4_t*>(a.out.data + int64_t{seq.start + static_cast<int>(token0 + on)} * a.out.row + to_head * a.out.head + column) = y;
+        };
+        const auto put = [&](float* part, int r, int column, float4_t v, float top, float s) {
+            store_partial(part + r * D + column, v[0], v[1]);
+            store_partial(part + r * D + column + 2, v[2], v[3]);
+            if (column == 0) store_partial(part + kRowBlock * D + 2 * r, top, s);
         };
         float* partial = a.partials + (2 * me + (from == 0 ? 1 : 0)) * kPartial;
         for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
             const int r = i / (D / 4), column = 4 * (i % (D / 4));
             float top = shared.top[0][r];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, shared.top[w][r]);
+            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, shared.top[w][r]);
             float4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
             float s = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const float f = weight_of(shared.top[w][r], top);
                 s += f * shared.sum[w][r];
                 v += f * *reinterpret_cast<const float4_t*>(&shared.out[w][r][column]);
             }
-            if (whole) {
-                write(r, column, v, s);
-            } else {
-                store_partial(partial + r * D + column, v[0], v[1]);
-                store_partial(partial + r * D + column + 2, v[2], v[3]);
-                if (column == 0) store_partial(partial + kRowBlock * D + 2 * r, top, s);
-            }
+            if (whole) write(r, column, v, s);
+            else put(partial, r, column, v, top, s);
         }
         if (!whole) {
-            // the first workgroup of the segment (its number names the counter) and the last
-            const int64_t segment_start = at - from, segment_end = segment_start + steps;
-            const int64_t w0 = ((segment_start + 1) * workers - 1) / total, w1 = (segment_end * workers - 1) / total;
-            const int parts = static_cast<int>(w1 - w0) + 1;
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // every thread's part is where the others can see it
-            __syncthreads();
-            if (threadIdx.x == 0)
-                shared.last = __hip_atomic_fetch_add(a.arrivals + w0, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
-            __syncthreads();
-            if (shared.last) {
-                const int columns = rows * (D / 4), teams = max(1, kThreads / columns);
-                for (int i = threadIdx.x; i < columns * teams; i += kThreads) {
-                    const int team = i / columns, of = i - team * columns, r = of / (D / 4), column = 4 * (of % (D / 4));
-                    float top = kMinusInf, s = 0.0f;
-                    float4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
-                    const auto part_at = [&](int p) { return a.partials + (2 * (w0 + p) + (p == 0 ? 1 : 0)) * kPartial; };
-                    constexpr int kAhead = 4;
-                    for (int p0 = team; p0 < parts; p0 += teams * kAhead) {
-                        float2 x[kAhead], y[kAhead], z[kAhead];
-#pragma unroll
-                        for (int j = 0; j < kAhead; ++j) {
-                            const float* from_part = part_at(min(p0 + j * teams, parts - 1));
-                            x[j] = load_partial(from_part + r * D + column);
-                            y[j] = load_partial(from_part + r * D + column + 2);
-                            z[j] = load_partial(from_part + kRowBlock * D + 2 * r);
-                        }
-#pragma unroll
-                        for (int j = 0; j < kAhead; ++j) {
-                            if (p0 + j * teams >= parts) break;
-                            const float both = fmaxf(top, z[j].x);
-                            const float f = weight_of(top, both), g = weight_of(z[j].x, both);
-                            s = f * s + g * z[j].y;
-                            v = f * v + g * float4_t{x[j].x, x[j].y, y[j].x, y[j].y};
-                            top = both;
-                        }
-                    }
-                    if (teams == 1) {
-                        write(r, column, v, s);
-                    } else {
-                        float* out = &shared.out[0][0][0] + i * 6;
-                        out[0] = top, out[1] = s, out[2] = v[0], out[3] = v[1], out[4] = v[2], out[5] = v[3];
-                    }
+            // The first workgroup of the segment, by whose number its counters go, and how many there are.  Up to kFan parts the last workgroup to arrive joins
+            // them; of more, every kFan neighbours are joined by the last of them to arrive, and the last of those joins the results: else one
+            // workgroup would read all parts alone (of 64 parts of 8 rows 262 KB).
+            const unsigned segment_start = at - from, w0 = owner_of(segment_start);
+            const int parts = owner_of(segment_start + steps - 1) - w0 + 1, mine = me - w0;
+            // Parts are written and read by agent-scope atomic operations, which pass the caches that are not coherent, and the counters count them only when they have
+            // arrived.  (A release and an acquire around the counters would write back and empty whole L2 caches: 3 times the kernel's time.)
+            const auto arrived_last = [&](int* counter, int all) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                if (threadIdx.x == 0) {
+                    shared.last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == all - 1;
+                    if (shared.last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // (for the next call)
                 }
-                if (teams > 1) {
-                    __syncthreads();
-                    for (int of = threadIdx.x; of < columns; of += kThreads) {
-                        const float* in = &shared.out[0][0][0];
-                        float top = kMinusInf;
-                        for (int k = 0; k < teams; ++k) top = fmaxf(top, in[(k * columns + of) * 6]);
-                        float s = 0.0f;
-                        float4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
-                        for (int k = 0; k < teams; ++k) {
-                            const float* p = in + (k * columns + of) * 6;
-                            const float f = weight_of(p[0], top);
-                            s += f * p[1];
-                            v += f * float4_t{p[2], p[3], p[4], p[5]};
-                        }
-                        write(of / (D / 4), 4 * (of % (D / 4)), v, s);
-                    }
+                __syncthreads();
+                return shared.last != 0;
+            };
+            const auto part_of = [&](int p) { return a.partials + (2 * (w0 + p) + (p == 0 ? 1 : 0)) * kPartial; };
+            const auto joint_of = [&](int g) { return a.partials + (2 * kAttendWorkgroups + w0 + g * kFan) * kPartial; };
+            const auto finish = [&](int r, int column, float4_t v, float, float s) { write(r, column, v, s); };
+            if (parts <= kFan) {
+                if (arrived_last(a.arrivals + w0, parts)) join<D, kThreads>(rows, parts, &shared.out[0][0][0], part_of, finish);
+            } else {
+                const int g = mine / kFan, groups = (parts + kFan - 1) / kFan;
+                if (arrived_last(a.arrivals + w0 + g * kFan, min(kFan, parts - g * kFan))) {
+                    join<D, kThreads>(rows, min(kFan, parts - g * kFan), &shared.out[0][0][0], [&](int p) { return part_of(g * kFan + p); },
+                                      [&](int r, int column, float4_t v, float top, float s) { put(joint_of(g), r, column, v, top, s); });
+                    if (arrived_last(a.arrivals + kAttendWorkgroups + w0, groups)) join<D, kThreads>(rows, groups, &shared.out[0][0][0], joint_of, finish);
                 }
-                if (threadIdx.x == 0) __hip_atomic_store(a.arrivals + w0, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
         }
         __syncthreads();       // (LDS is free again)
@@ -658,10 +726,10 @@ gqsa_status_t cache_allocate(gqsa_cache* c)
     c->d_pages = static_cast<uint8_t*>(p);
     GQSA_HIP(hipMalloc(&p, static_cast<size_t>(c->partial_floats()) * 4));
     c->d_partials = static_cast<float*>(p);
-    GQSA_HIP(hipMalloc(&p, kAttendWorkgroups * 4));
+    GQSA_HIP(hipMalloc(&p, kAttendWorkgroups * 2 * 4));
     c->d_arrivals = static_cast<int32_t*>(p);
     GQSA_HIP(hipMemset(c->d_pages, 0, static_cast<size_t>(c->device_bytes())));
-    GQSA_HIP(hipMemset(c->d_arrivals, 0, kAttendWorkgroups * 4));
+    GQSA_HIP(hipMemset(c->d_arrivals, 0, kAttendWorkgroups * 2 * 4));
     GQSA_HIP(hipDeviceSynchronize());
     return GQSA_OK;
 }
@@ -708,14 +776,18 @@ gqsa_status_t cache_attend(gqsa_cache* c, const Heads& q, int q_heads, const Seq
 {
     if (gqsa_status_t st = on_device(c)) return st;
     const int per = q_heads / c->kv_heads;
-    const AttendArgs a{pool_of(c), q, out, seqs, c->d_partials, c->d_arrivals, per, scale * 1.44269504088896341f};
-    // no more workgroups than there can be steps
+    const AttendArgs a{pool_of(c), q, out, seqs, c->d_partials, c->d_arrivals, per,
+                       // (not 0, so that a masked score stays -infinity: 1e-30 leaves every weight at 1)
+                       std::max(std::fabs(scale) * 1.44269504088896341f, 1e-30f), scale < 0.0f};
+    // No more workgroups than there can be steps.  (The kernel counts them, and rows of a group, in 32 bits.)
+    if (seqs.n_rows * per > (1 << 30)) return GQSA_ERR_SHAPE;
     const double blocks = (static_cast<double>(seqs.n_rows) * per / kRowBlock + seqs.n_seqs) * c->kv_heads;
-    const double steps = static_cast<double>(seqs.max_pages) * c->page_tokens / (kStepTiles * kTileTokens) + 1.0;
-    const unsigned grid = static_cast<unsigned>(std::max(1.0, std::min<double>(kAttendWorkgroups, blocks * steps)));
+    const double steps = blocks * (static_cast<double>(seqs.max_pages) * c->page_tokens / (kAttendWaves * kTileTokens) + 1.0);
+    if (steps > INT_MAX) return GQSA_ERR_SHAPE;
+    const unsigned grid = static_cast<unsigned>(std::max(1.0, std::min<double>(kAttendWorkgroups, steps)));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (c->head_dim == 128) hipLaunchKernelGGL(attend_kernel<128>, dim3(grid), dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL(attend_kernel<64>, dim3(grid), dim3(kThreads), 0, s, a);
+    if (c->head_dim == 128) hipLaunchKernelGGL((attend_kernel<128, kAttendWaves>), dim3(grid), dim3(64 * kAttendWaves), 0, s, a);
+    else hipLaunchKernelGGL((attend_kernel<64, kAttendWaves>), dim3(grid), dim3(64 * kAttendWaves), 0, s, a);
     GQSA_HIP(hipGetLastError());
     return GQSA_OK;
 }

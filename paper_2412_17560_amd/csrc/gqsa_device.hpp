@@ -15,47 +15,63 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr float kMinusInf = -__builtin_inff();
 
-// Sum over the lanes up to and including this one.
-__device__ __forceinline__ int64_t running_sum(int64_t v, int lane)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// (sums that would pass 2^32 stay at its end: what the arrays on the device say is not trusted to be sound)
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ unsigned add_from(unsigned v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t other = __shfl_up(v, d);
-        if (lane >= d) v += other;
-    }
-    return v;
+    return __builtin_elementwise_add_sat(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CONTROL, ROWS, 0xF, false)));
 }
 
-// Of units dealt to the sequences in order, count(b) to sequence b: the sequence that unit `unit` belongs to and the unit's number there;
-// false if there are fewer units.  Called by whole wavefronts.
-template <typename Count>
-__device__ __forceinline__ bool locate(int n_seqs, int64_t unit, int lane, Count&& count, int* b, int64_t* within)
+// Sum over the lanes up to and including this one: within the rows of 16 lanes by shifts, then the rows' sums handed on.
+__device__ __forceinline__ unsigned running_sum(unsigned v)
 {
-    int64_t before = 0;
-    for (int b0 = 0; b0 < n_seqs; b0 += 64) {
-        const int64_t mine = b0 + lane < n_seqs ? count(b0 + lane) : 0;
-        const int64_t upto = running_sum(mine, lane);
-        const unsigned long long past = __ballot(before + upto > unit);
-        if (past) {
-            const int who = __ffsll(past) - 1;
-            *b = b0 + who;
-            *within = unit - before - __shfl(upto - mine, who);
-            return true;
+    v = add_from<0x111, 0xF>(v);        // from the lane 1 before
+    v = add_from<0x112, 0xF>(v);        // 2
+    v = add_from<0x114, 0xF>(v);        // 4
+    v = add_from<0x118, 0xF>(v);        // 8
+    v = add_from<0x142, 0xA>(v);        // lane 15 of the row before, into the second and the fourth row
+    return add_from<0x143, 0xC>(v);     // lane 31, into the third and the fourth
+}
+
+// Units dealt to the sequences in order, count(b) to sequence b: how many there are (0 if it is 2^31 or more, which no sound call has), and to which sequence
+// a unit belongs and as the how manieth.  Called by whole wavefronts; sequences beyond the first 64 are counted again by locate().
+template <typename Count>
+struct Deal {
+    int n_seqs, lane;
+    Count count;
+    unsigned own, upto, of_first, total;
+
+    __device__ __forceinline__ Deal(int n_seqs_, int lane_, Count count_) : n_seqs(n_seqs_), lane(lane_), count(count_)
+    {
+        own = lane < n_seqs ? count(lane) : 0u;
+        upto = running_sum(own);
+        total = of_first = last(upto);
+        for (int b0 = 64; b0 < n_seqs; b0 += 64)
+            total = __builtin_elementwise_add_sat(total, last(running_sum(b0 + lane < n_seqs ? count(b0 + lane) : 0u)));
+        if (total > 0x7FFFFFFFu) total = 0;
+    }
+
+    __device__ static __forceinline__ unsigned last(unsigned v) { return __builtin_amdgcn_readlane(static_cast<int>(v), 63); }
+
+    // unit < total
+    __device__ __forceinline__ void locate(unsigned unit, int* b, int* within) const
+    {
+        unsigned before = 0, sum = upto, mine = own, all = of_first;
+        int b0 = 0;
+        while (unit >= before + all && b0 + 64 < n_seqs) {
+            before += all;
+            b0 += 64;
+            mine = b0 + lane < n_seqs ? count(b0 + lane) : 0u;
+            sum = running_sum(mine);
+            all = last(sum);
         }
-        before += __shfl(upto, 63);
+        const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + sum > unit));
+        *b = b0 + who;
+        *within = unit - before - __builtin_amdgcn_readlane(static_cast<int>(sum - mine), who);
     }
-    return false;
-}
-
-template <typename Count>
-__device__ __forceinline__ int64_t total_of(int n_seqs, int lane, Count&& count)
-{
-    int64_t sum = 0;
-    for (int b = lane; b < n_seqs; b += 64) sum += count(b);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    return sum;
-}
+};
 
 // Values that are not finite, where a mask hides some of them from some rows: a product with a weight of 0 would make them NaN for every row.  The
 // product then takes `finite_part` and a second one counts, for each row and element, the +infinities, -infinities and NaN that the row sees.

@@ -88,21 +88,20 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
     };
     const auto blocks_of = [&](int b) {
         int start;
-        return static_cast<int64_t>((rows_of(c.q_starts, c.n_q_rows, b, &start) + kBlockRows - 1) / kBlockRows);
+        return static_cast<unsigned>(rows_of(c.q_starts, c.n_q_rows, b, &start) + kBlockRows - 1) / kBlockRows;
     };
     // Heads vary fastest, those of a group on one XCD (workgroup i runs on XCD i % 8), the last blocks of a sequence -- those with the
     // most keys -- come first.
-    const int slot = blockIdx.x / c.q_heads, of = blockIdx.x % c.q_heads;
+    const unsigned slot = blockIdx.x / static_cast<unsigned>(c.q_heads), of = blockIdx.x % static_cast<unsigned>(c.q_heads);
     const int head = c.q_heads % 8 == 0 ? of % 8 * (c.q_heads / 8) + of / 8 : of;
-    const int64_t total = total_of(c.n_seqs, lane, blocks_of);
-    int b;
-    int64_t block;
-    if (slot >= total || !locate(c.n_seqs, total - 1 - slot, lane, blocks_of, &b, &block)) return;
-    b = __builtin_amdgcn_readfirstlane(b);
+    const Deal deal(c.n_seqs, lane, blocks_of);
+    if (slot >= deal.total) return;
+    int b, block;
+    deal.locate(deal.total - 1 - slot, &b, &block);
     int q_start, k_start;
     const int n_q = rows_of(c.q_starts, c.n_q_rows, b, &q_start), n_k = rows_of(c.k_starts, c.n_k_rows, b, &k_start);
     const int behind = n_k - n_q;                    // row r sees keys 0 .. r + behind
-    const int row0 = __builtin_amdgcn_readfirstlane(static_cast<int>(block)) * kBlockRows, wave_row0 = row0 + wave * kWaveRows;
+    const int row0 = block * kBlockRows, wave_row0 = row0 + wave * kWaveRows;
     const int row = wave_row0 + (lane & 31);
     const int sees = row + behind + 1;
     const int keys = max(min(n_q, row0 + kBlockRows) + behind, 0);                               // that some row of the block sees
