@@ -77,11 +77,11 @@ struct Unit {
 
 __device__ __forceinline__ bool unit_of(const CopyArgs& a, Unit* u)
 {
-    const Deal deal(a.seqs.n_seqs, threadIdx.x & 63, [&](int s) { return static_cast<unsigned>(tiles_of_rows(sequence(a.seqs, a.pool.page_shift, s))); });
+    const auto deal = deal_out<Sequence>(a.seqs.n_seqs, threadIdx.x & 63, [&](int s) { return sequence(a.seqs, a.pool.page_shift, s); },
+                                         [](const Sequence& q) { return static_cast<unsigned>(tiles_of_rows(q)); });
     if (blockIdx.x >= deal.total) return false;
     int b, within;
-    deal.locate(blockIdx.x, &b, &within);
-    u->seq = sequence(a.seqs, a.pool.page_shift, b);
+    u->seq = deal.locate(blockIdx.x, &b, &within);
     u->tile = ((u->seq.length - u->seq.rows) >> 5) + within;
     u->head = blockIdx.y;
     u->page = -1;
@@ -95,7 +95,7 @@ __device__ __forceinline__ bool unit_of(const CopyArgs& a, Unit* u)
 template <int N>
 struct Quantised {
     _Float16 low, step;
-    uint8_t code[N];
+    uint32_t code[N];
 };
 
 // N elements of a group whose other elements are with the neighbouring 32 / N - 1 lanes.
@@ -120,32 +120,51 @@ __device__ __forceinline__ Quantised<N> quantise(const half8_t (&x)[N / 8])
     uint16_t step_bits = __builtin_bit_cast(uint16_t, static_cast<_Float16>(bad ? 0.0f : (high - low) / 15.0f));
     if (low + 15.0f * static_cast<float>(__builtin_bit_cast(_Float16, step_bits)) >= 65520.0f) --step_bits;       // (what rounds to infinity)
     q.step = __builtin_bit_cast(_Float16, step_bits);
-    const float step = static_cast<float>(q.step);
+    // (x - low) / step as one rounded division: with the rounded reciprocal, a product, its exact remainder and one correction.  The corrected
+    // quotient is off by 2^-23 of its last place before it is rounded, and no quotient by a number of 11 bits lies that near to the middle
+    // between two fp32 numbers, so the rounding is the division's.
+    const float step = static_cast<float>(q.step), divisor = step > 0.0f ? step : 1.0f, inverse = 1.0f / divisor;
+    const float highest = step > 0.0f ? 15.0f : 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float v = static_cast<float>(x[i / 8][i % 8]);
-        q.code[i] = step > 0.0f ? static_cast<uint8_t>(fminf(__builtin_rintf((v - low) / step), 15.0f)) : 0;
+        const float over = static_cast<float>(x[i / 8][i % 8]) - low, first = over * inverse;
+        const float quotient = __builtin_fmaf(__builtin_fmaf(-first, divisor, over), inverse, first);
+        q.code[i] = static_cast<uint32_t>(fmaxf(fminf(__builtin_rintf(quotient), highest), 0.0f));
     }
     return q;
 }
 
-// One workgroup per tile that gets rows, and head: 8 threads to a token.  A word of key codes belongs to one token; one of value codes to 8
-// tokens, so those are put together in LDS, and a word that keeps earlier tokens is read first (nobody else writes the tile).
+// One workgroup per tile that gets rows, and head: 8 threads to a token.  The tile is put together in LDS -- a word of key codes is of one token, but one of
+// value codes of 8 -- and written in runs of 16 bytes; of a tile that keeps earlier tokens, only the new ones' words and halves are
+// written, and words of value codes that they share are read first (nobody else writes the tile).
 template <int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(CopyArgs a)
 {
     constexpr int kOwn = D / 8;                    // elements of a token per thread
     constexpr int kParameters = 32 * D;            // where the parameters start in a tile
-    __shared__ uint8_t v_codes[kTileTokens][D];
+    __shared__ alignas(16) uint8_t image[tile_bytes(D)];
+    __shared__ alignas(16) uint8_t v_codes[kTileTokens][D + 4];
     Unit u;
     if (!unit_of(a, &u) || u.page < 0) return;
     uint8_t* tile = a.pool.tile<D>(u.page, u.head, u.tile);
-    const int first = u.seq.length - u.seq.rows;   // the rows' first token
-    const auto is_new = [&](int t) { const int token = u.tile * kTileTokens + t; return token >= first && token < u.seq.length; };
+    // of the tile's tokens, from .. to - 1 are new
+    const int first = u.seq.length - u.seq.rows - u.tile * kTileTokens;       // the rows' first token
+    const int from = max(first, 0), to = min(u.seq.length - u.tile * kTileTokens, kTileTokens);
 
-    const int t = threadIdx.x >> 3, part = threadIdx.x & 7;
-    if (is_new(t)) {
-        const int64_t row = u.seq.start + (u.tile * kTileTokens + t - first);
+    const int t = threadIdx.x >> 3, part = threadIdx.x & 7, group = part * kOwn / kGroupChannels;
+    const bool leads = part % (kGroupChannels / kOwn) == 0, fresh = t >= from && t < to;
+    const bool all = from == 0 && to == kTileTokens;
+    constexpr int kWords = D / 16 * 64 / kThreads;      // words of value codes per thread
+    uint32_t old[kWords] = {};
+    if (!all) {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {              // (whether wanted or not: ahead of everything else)
+            const int at = i * kThreads + threadIdx.x;
+            old[i] = *reinterpret_cast<const uint32_t*>(tile + 16 * D + word_offset(at >> 6, at & 63));
+        }
+    }
+    if (fresh) {
+        const int64_t row = u.seq.start + (t - first);
         const uint16_t* k_at = a.k.data + row * a.k.row + u.head * a.k.head + part * kOwn;
         const uint16_t* v_at = a.v.data + row * a.v.row + u.head * a.v.head + part * kOwn;
         half8_t x[kOwn / 8], y[kOwn / 8];
@@ -154,46 +173,61 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CopyArgs a)
             x[i] = reinterpret_cast<const half8_t*>(k_at)[i];
             y[i] = reinterpret_cast<const half8_t*>(v_at)[i];
         }
-        const int group = part * kOwn / kGroupChannels;
-        const bool leads = part % (kGroupChannels / kOwn) == 0;
         const Quantised<kOwn> k = quantise<kOwn>(x);
 #pragma unroll
         for (int i = 0; i < kOwn / 8; ++i) {
             uint32_t word = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) word |= uint32_t{k.code[8 * i + e]} << nibble(e);
+            for (int e = 0; e < 8; ++e) word |= k.code[8 * i + e] << nibble(e);
             const int quad = (part * kOwn + 8 * i) % kGroupChannels / 8;
-            const int w = (t >> 4) * (D / 32) + group;
-            *reinterpret_cast<uint32_t*>(tile + word_offset(w, quad * 16 + (t & 15))) = word;
+            *reinterpret_cast<uint32_t*>(image + word_offset((t >> 4) * (D / 32) + group, quad * 16 + (t & 15))) = word;
         }
-        if (leads) {
-            const half2_t both = {k.low, k.step};
-            *reinterpret_cast<half2_t*>(tile + kParameters + (t * (D / 32) + group) * 4) = both;
-        }
+        if (leads) *reinterpret_cast<half2_t*>(image + kParameters + (t * (D / 32) + group) * 4) = half2_t{k.low, k.step};
         const Quantised<kOwn> v = quantise<kOwn>(y);
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) v_codes[t][part * kOwn + i] = v.code[i];
+        for (int i = 0; i < kOwn; i += 4)
+            *reinterpret_cast<uint32_t*>(&v_codes[t][part * kOwn + i]) =
+                v.code[i] | v.code[i + 1] << 8 | v.code[i + 2] << 16 | v.code[i + 3] << 24;
         if (leads) {
             const int quad = (t >> 2) & 3, slot = (t & 3) + (t >> 4) * 4;
-            _Float16* at = reinterpret_cast<_Float16*>(tile + kParameters + 4 * D + (group * 4 + quad) * 32) + slot;
+            _Float16* at = reinterpret_cast<_Float16*>(image + kParameters + 4 * D + (group * 4 + quad) * 32) + slot;
             at[0] = v.step;
             at[8] = v.low;
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < D / 16 * 64; i += kThreads) {
-        const int c = i >> 6, l = i & 63, quad = l >> 4;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+        const int c = (i * kThreads + threadIdx.x) >> 6, l = threadIdx.x & 63, quad = l >> 4;
         uint32_t word = 0, kept = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int token = slot_token(quad, e);
-            if (is_new(token)) word |= uint32_t{v_codes[token][16 * c + (l & 15)]} << nibble(e);
-            else kept |= 15u << nibble(e);
+            const bool is_new = token >= from && token < to;
+            word |= (is_new ? uint32_t{v_codes[token][16 * c + (l & 15)]} : 0u) << nibble(e);
+            kept |= (is_new ? 0u : 15u) << nibble(e);
         }
-        if (kept == ~0u) continue;
-        uint32_t* at = reinterpret_cast<uint32_t*>(tile + 16 * D + word_offset(c, l));
-        if (kept) word |= *at & kept;
-        *at = word;
+        const int at = 16 * D + word_offset(c, l);
+        if (all) *reinterpret_cast<uint32_t*>(image + at) = word;
+        else if (kept != ~0u) *reinterpret_cast<uint32_t*>(tile + at) = word | (old[i] & kept);
+    }
+    if (all) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < tile_bytes(D) / 16; i += kThreads)
+            reinterpret_cast<u32x4_t*>(tile)[i] = reinterpret_cast<const u32x4_t*>(image)[i];
+    } else if (fresh) {
+#pragma unroll
+        for (int i = 0; i < kOwn / 8; ++i) {
+            const int at = word_offset((t >> 4) * (D / 32) + group, (part * kOwn + 8 * i) % kGroupChannels / 8 * 16 + (t & 15));
+            *reinterpret_cast<uint32_t*>(tile + at) = *reinterpret_cast<const uint32_t*>(image + at);
+        }
+        if (leads) {
+            const int k_at = kParameters + (t * (D / 32) + group) * 4;
+            const int v_at = kParameters + 4 * D + (group * 4 + ((t >> 2) & 3)) * 32 + 2 * ((t & 3) + (t >> 4) * 4);
+            *reinterpret_cast<uint32_t*>(tile + k_at) = *reinterpret_cast<const uint32_t*>(image + k_at);
+            *reinterpret_cast<uint16_t*>(tile + v_at) = *reinterpret_cast<const uint16_t*>(image + v_at);
+            *reinterpret_cast<uint16_t*>(tile + v_at + 16) = *reinterpret_cast<const uint16_t*>(image + v_at + 16);
+        }
     }
 }
 
@@ -202,27 +236,33 @@ __global__ __launch_bounds__(kThreads) void read_kernel(CopyArgs a)
 {
     constexpr int kOwn = D / 8;
     constexpr int kParameters = 32 * D;
+    __shared__ alignas(16) uint8_t image[tile_bytes(D)];
     Unit u;
     if (!unit_of(a, &u)) return;
+    if (u.page >= 0) {
+        const uint8_t* tile = a.pool.tile<D>(u.page, u.head, u.tile);
+        for (int i = threadIdx.x; i < tile_bytes(D) / 16; i += kThreads)
+            reinterpret_cast<u32x4_t*>(image)[i] = reinterpret_cast<const u32x4_t*>(tile)[i];
+    }
+    __syncthreads();
     const int first = u.seq.length - u.seq.rows;
     const int t = threadIdx.x >> 3, part = threadIdx.x & 7;
     const int token = u.tile * kTileTokens + t;
     if (token < first || token >= u.seq.length) return;
     half8_t x[kOwn / 8] = {}, y[kOwn / 8] = {};
     if (u.page >= 0) {
-        const uint8_t* tile = a.pool.tile<D>(u.page, u.head, u.tile);
         const int group = part * kOwn / kGroupChannels, quad = (t >> 2) & 3, slot = (t & 3) + (t >> 4) * 4;
-        const half2_t k = *reinterpret_cast<const half2_t*>(tile + kParameters + (t * (D / 32) + group) * 4);
-        const _Float16* v = reinterpret_cast<const _Float16*>(tile + kParameters + 4 * D + (group * 4 + quad) * 32) + slot;
+        const half2_t k = *reinterpret_cast<const half2_t*>(image + kParameters + (t * (D / 32) + group) * 4);
+        const _Float16* v = reinterpret_cast<const _Float16*>(image + kParameters + 4 * D + (group * 4 + quad) * 32) + slot;
         const _Float16 v_step = v[0], v_low = v[8];
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
             const int element = part * kOwn + i;
             const uint32_t kw = *reinterpret_cast<const uint32_t*>(
-                tile + word_offset((t >> 4) * (D / 32) + group, element % kGroupChannels / 8 * 16 + (t & 15)));
-            const uint32_t vw = *reinterpret_cast<const uint32_t*>(tile + 16 * D + word_offset(element / 16, quad * 16 + element % 16));
+                image + word_offset((t >> 4) * (D / 32) + group, element % kGroupChannels / 8 * 16 + (t & 15)));
+            const uint32_t vw = *reinterpret_cast<const uint32_t*>(image + 16 * D + word_offset(element / 16, quad * 16 + element % 16));
             x[i / 8][i % 8] = __builtin_fmaf16(static_cast<_Float16>(static_cast<float>(kw >> nibble(i % 8) & 15u)), k[1], k[0]);
-            y[i / 8][i % 8] = __builtin_fmaf16(static_cast<_Float16>(static_cast<float>(vw >> nibble(slot) & 15u)), v_step, v_low);
+            y[i / 8][i % 8] = __builtin_fmaf16(static_cast<_Float16>(static_cast<float>(vw >> (8 * (slot & 3) + 4 * (slot >> 2)) & 15u)), v_step, v_low);
         }
     }
     const int64_t row = u.seq.start + (token - first);
@@ -530,8 +570,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
     const unsigned per = a.heads_per_group;
     const auto blocks_of = [&](const Sequence& q) { return static_cast<int>((static_cast<unsigned>(q.rows) * per + kRowBlock - 1) / kRowBlock); };
     const auto steps_of = [](const Sequence& q) { return max((q.length + kStepTiles * kTileTokens - 1) / (kStepTiles * kTileTokens), 1); };
-    const Deal deal(a.seqs.n_seqs, lane, [&](int b) {
-        const Sequence q = sequence(a.seqs, a.pool.page_shift, b);
+    const auto deal = deal_out<Sequence>(a.seqs.n_seqs, lane, [&](int b) { return sequence(a.seqs, a.pool.page_shift, b); }, [&](const Sequence& q) {
         return static_cast<unsigned>(min(static_cast<int64_t>(blocks_of(q)) * steps_of(q) * a.pool.kv_heads, int64_t{INT_MAX}));
     });
     const unsigned total = deal.total, workers = min(gridDim.x, total), me = blockIdx.x;
@@ -545,9 +584,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
     int at = start_of(me);
     const int end = start_of(me + 1);
     int b, within;
-    deal.locate(at, &b, &within);
-
-    Sequence seq = sequence(a.seqs, a.pool.page_shift, b);
+    Sequence seq = deal.locate(at, &b, &within);
     while (at < end) {
         const int blocks = blocks_of(seq), steps = steps_of(seq);
         if (within >= blocks * steps * a.pool.kv_heads) {       // (on to the next sequence that has rows)

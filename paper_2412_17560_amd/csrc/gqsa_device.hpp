@@ -35,43 +35,56 @@ __device__ __forceinline__ unsigned running_sum(unsigned v)
     return add_from<0x143, 0xC>(v);     // lane 31, into the third and the fourth
 }
 
-// Units dealt to the sequences in order, count(b) to sequence b: how many there are (0 if it is 2^31 or more, which no sound call has), and to which sequence
-// a unit belongs and as the how manieth.  Called by whole wavefronts; sequences beyond the first 64 are counted again by locate().
-template <typename Count>
+// Units dealt to the sequences in order, count(seq) to a sequence that load(b) has fetched (a struct of three ints): how many there are (0 if it is 2^31 or
+// more, which no sound call has), and to which sequence a unit belongs and as the how manieth.  Lane l holds the l-th sequence, so that
+// no load waits for another.  Called by whole wavefronts; sequences beyond the first 64 are fetched again by locate().
+template <typename Seq, typename Load, typename Count>
 struct Deal {
     int n_seqs, lane;
+    Load load;
     Count count;
+    Seq seq;
     unsigned own, upto, of_first, total;
 
-    __device__ __forceinline__ Deal(int n_seqs_, int lane_, Count count_) : n_seqs(n_seqs_), lane(lane_), count(count_)
+    __device__ __forceinline__ Deal(int n_seqs_, int lane_, Load load_, Count count_) : n_seqs(n_seqs_), lane(lane_), load(load_), count(count_)
     {
-        own = lane < n_seqs ? count(lane) : 0u;
+        seq = load(min(lane, n_seqs - 1));
+        own = lane < n_seqs ? count(seq) : 0u;
         upto = running_sum(own);
         total = of_first = last(upto);
         for (int b0 = 64; b0 < n_seqs; b0 += 64)
-            total = __builtin_elementwise_add_sat(total, last(running_sum(b0 + lane < n_seqs ? count(b0 + lane) : 0u)));
+            total = __builtin_elementwise_add_sat(total, last(running_sum(b0 + lane < n_seqs ? count(load(b0 + lane)) : 0u)));
         if (total > 0x7FFFFFFFu) total = 0;
     }
 
     __device__ static __forceinline__ unsigned last(unsigned v) { return __builtin_amdgcn_readlane(static_cast<int>(v), 63); }
 
     // unit < total
-    __device__ __forceinline__ void locate(unsigned unit, int* b, int* within) const
+    __device__ __forceinline__ Seq locate(unsigned unit, int* b, int* within) const
     {
         unsigned before = 0, sum = upto, mine = own, all = of_first;
+        Seq held = seq;
         int b0 = 0;
         while (unit >= before + all && b0 + 64 < n_seqs) {
             before += all;
             b0 += 64;
-            mine = b0 + lane < n_seqs ? count(b0 + lane) : 0u;
+            held = load(min(b0 + lane, n_seqs - 1));
+            mine = b0 + lane < n_seqs ? count(held) : 0u;
             sum = running_sum(mine);
             all = last(sum);
         }
         const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + sum > unit));
         *b = b0 + who;
         *within = unit - before - __builtin_amdgcn_readlane(static_cast<int>(sum - mine), who);
+        return {__builtin_amdgcn_readlane(held.start, who), __builtin_amdgcn_readlane(held.rows, who), __builtin_amdgcn_readlane(held.length, who)};
     }
 };
+
+template <typename Seq, typename Load, typename Count>
+__device__ __forceinline__ Deal<Seq, Load, Count> deal_out(int n_seqs, int lane, Load load, Count count)
+{
+    return {n_seqs, lane, load, count};
+}
 
 // Values that are not finite, where a mask hides some of them from some rows: a product with a weight of 0 would make them NaN for every row.  The
 // product then takes `finite_part` and a second one counts, for each row and element, the +infinities, -infinities and NaN that the row sees.

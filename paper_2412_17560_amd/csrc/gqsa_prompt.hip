@@ -81,25 +81,22 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
     __shared__ PromptShared<D> shared;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
 
-    const auto rows_of = [](const int32_t* starts, int64_t n, int b, int* start) {
-        const int most = static_cast<int>(n);
-        *start = min(max(starts[b], 0), most);
-        return max(min(starts[b + 1], most) - *start, 0);
+    struct Prompt {
+        int start, rows, length;       // query rows, and where they start; keys
     };
-    const auto blocks_of = [&](int b) {
-        int start;
-        return static_cast<unsigned>(rows_of(c.q_starts, c.n_q_rows, b, &start) + kBlockRows - 1) / kBlockRows;
-    };
+    const auto start_of = [](const int32_t* starts, int64_t n, int b) { return min(max(starts[b], 0), static_cast<int>(n)); };
+    const auto rows_of = [&](const int32_t* starts, int64_t n, int b) { return max(min(starts[b + 1], static_cast<int>(n)) - start_of(starts, n, b), 0); };
     // Heads vary fastest, those of a group on one XCD (workgroup i runs on XCD i % 8), the last blocks of a sequence -- those with the
     // most keys -- come first.
     const unsigned slot = blockIdx.x / static_cast<unsigned>(c.q_heads), of = blockIdx.x % static_cast<unsigned>(c.q_heads);
     const int head = c.q_heads % 8 == 0 ? of % 8 * (c.q_heads / 8) + of / 8 : of;
-    const Deal deal(c.n_seqs, lane, blocks_of);
+    const auto deal = deal_out<Prompt>(c.n_seqs, lane, [&](int b) {
+        return Prompt{start_of(c.q_starts, c.n_q_rows, b), rows_of(c.q_starts, c.n_q_rows, b), rows_of(c.k_starts, c.n_k_rows, b)};
+    }, [](const Prompt& p) { return static_cast<unsigned>(p.rows + kBlockRows - 1) / kBlockRows; });
     if (slot >= deal.total) return;
     int b, block;
-    deal.locate(deal.total - 1 - slot, &b, &block);
-    int q_start, k_start;
-    const int n_q = rows_of(c.q_starts, c.n_q_rows, b, &q_start), n_k = rows_of(c.k_starts, c.n_k_rows, b, &k_start);
+    const Prompt prompt = deal.locate(deal.total - 1 - slot, &b, &block);
+    const int q_start = prompt.start, n_q = prompt.rows, n_k = prompt.length, k_start = start_of(c.k_starts, c.n_k_rows, b);
     const int behind = n_k - n_q;                    // row r sees keys 0 .. r + behind
     const int row0 = block * kBlockRows, wave_row0 = row0 + wave * kWaveRows;
     const int row = wave_row0 + (lane & 31);
