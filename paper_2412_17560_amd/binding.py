@@ -454,16 +454,38 @@ def gqsa_stream_read(buf, sink, stream=None) -> None:
 
 # ----------------------------------------------------------------------------- between the q/k/v and the o product
 
+# These calls, too, are bound by their host work where the kernels take a few microseconds: an attribute of a tensor costs 0.05 to 0.08 us, so each
+# is asked for once (norm and rotation of one row: 11.1 us a call with the helpers above, 9.4 with these).
+
 def _heads(t, what: str):
-    """(pointer, distance between rows, distance between heads) of a float16 device tensor [rows, heads, head_dim] whose heads are
-    contiguous; the other two dimensions may be strided."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float16:
-        raise ValueError(f"{what} must be a float16 device tensor")
-    if t.dim() != 3 or t.stride(2) != 1:
-        raise ValueError(f"{what} must be [rows, heads, head_dim] with contiguous heads")
-    rows, heads, _ = t.shape         # (torch lets the distance of a dimension of size 1 be anything)
-    return t.data_ptr(), t.stride(0) if rows > 1 else 0, t.stride(1) if heads > 1 else 0
+    """(pointer, distance between rows, distance between heads, rows, heads, head_dim) of a float16 device tensor [rows, heads, head_dim]
+    whose heads are contiguous; the other two dimensions may be strided."""
+    try:
+        rows, heads, dim = t.shape
+        row, head, one = t.stride()
+        good = t.is_cuda and t.dtype is _half()
+    except (AttributeError, TypeError, ValueError):
+        good, one = False, 1
+    if not good or one != 1:
+        raise ValueError(f"{what} must be a float16 device tensor [rows, heads, head_dim] with contiguous heads")
+    # (torch lets the distance of a dimension of size 1 be anything)
+    return t.data_ptr(), row if rows > 1 else 0, head if heads > 1 else 0, rows, heads, dim
+
+
+def _half():
+    dtype = _DTYPES.get("torch.float16")
+    if dtype is None:
+        import torch
+        dtype = _DTYPES.setdefault("torch.float16", torch.float16)
+    return dtype
+
+
+def _flat(t, what: str, dtype_name: str = "torch.int32"):
+    """(pointer, shape) of a contiguous device tensor of that dtype."""
+    dtype = _DTYPES.get(dtype_name)
+    if dtype is None or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        return _dev_ptr(t, dtype_name, what), t.shape         # (which says what is wrong, if anything is)
+    return t.data_ptr(), t.shape
 
 
 def _like(x, stream):
@@ -482,36 +504,42 @@ def gqsa_qk_norm_rotate(q, k, positions, table, q_weight=None, k_weight=None, ep
     """Norms of queries [rows, q_heads, head_dim] and keys [rows, k_heads, head_dim] per head (weights float16 [head_dim] or None: no norm)
     and their rotation: positions int32 [rows], table float32 [n_positions, rotary_dim / 2, 2] (cosine, sine), or both None: no
     rotation.  k None: queries only.  q_out = q, k_out = k: in place.  Returns (q_out, k_out)."""
-    q_at = _heads(q, "q")
-    rows, q_heads, dim = q.shape
+    q_at, q_row, q_head, rows, q_heads, dim = _heads(q, "q")
     if q_out is None:
         q_out = _like(q, stream)
-    if q_out.shape != q.shape:
+    qo_at, qo_row, qo_head, *shape = _heads(q_out, "q_out")
+    if shape != [rows, q_heads, dim]:
         raise ValueError("q_out must have the shape of q")
-    k_heads, k_at, k_out_at = 0, (None, 0, 0), (None, 0, 0)
+    k_at, k_row, k_head, k_heads, ko_at, ko_row, ko_head = None, 0, 0, 0, None, 0, 0
     if k is not None:
-        k_at = _heads(k, "k")
-        k_heads = k.shape[1]
+        k_at, k_row, k_head, k_rows, k_heads, k_dim = _heads(k, "k")
         if k_out is None:
             k_out = _like(k, stream)
-        if k.shape[0] != rows or k.shape[2] != dim or k_out.shape != k.shape:
+        ko_at, ko_row, ko_head, *shape = _heads(k_out, "k_out")
+        if k_rows != rows or k_dim != dim or shape != [rows, k_heads, dim]:
             raise ValueError("k must be [rows, k_heads, head_dim] and k_out as k")
-        k_out_at = _heads(k_out, "k_out")
     n_positions = rotary = 0
+    table_at = positions_at = None
     if table is not None:
-        if table.dim() != 3 or table.shape[2] != 2 or positions is None or positions.shape != (rows,):
+        table_at, shape = _flat(table, "table", "torch.float32")
+        n_positions, half, two = shape if len(shape) == 3 else (0, 0, 0)
+        if two != 2 or positions is None:
             raise ValueError("table must be [n_positions, rotary_dim / 2, 2] and positions [rows]")
-        n_positions, rotary = table.shape[0], 2 * table.shape[1]
-    for w in (q_weight, k_weight):
-        if w is not None and w.shape != (dim,):
-            raise ValueError("norm weights must be [head_dim]")
+        positions_at, shape = _flat(positions, "positions")
+        if shape != (rows,):
+            raise ValueError("positions must be [rows]")
+        rotary = 2 * half
+    weights = []
+    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        w_at = None
+        if w is not None:
+            w_at, shape = _flat(w, what, "torch.float16")
+            if shape != (dim,):
+                raise ValueError("norm weights must be [head_dim]")
+        weights.append(w_at)
     _check(_lib().gqsa_qk_norm_rotate(
-        *q_at, q_heads, *k_at, k_heads, rows, dim,
-        None if q_weight is None else _dev_ptr(q_weight, "torch.float16", "q_weight"),
-        None if k_weight is None else _dev_ptr(k_weight, "torch.float16", "k_weight"), eps,
-        _dev_ptr(table, "torch.float32", "table") if rotary else None, n_positions, rotary, int(interleaved),
-        _dev_ptr(positions, "torch.int32", "positions") if rotary else None,
-        *_heads(q_out, "q_out"), *k_out_at, _stream_ptr(stream)), "gqsa_qk_norm_rotate")
+        q_at, q_row, q_head, q_heads, k_at, k_row, k_head, k_heads, rows, dim, *weights, eps, table_at, n_positions, rotary, int(interleaved),
+        positions_at, qo_at, qo_row, qo_head, ko_at, ko_row, ko_head, _stream_ptr(stream)), "gqsa_qk_norm_rotate")
     return q_out, k_out
 
 
@@ -550,48 +578,52 @@ def gqsa_cache_free(c: GqsaCache) -> None:
 
 def _sequences(pages, lengths, row_starts):
     """pages int32 [n_seqs, max_pages], lengths int32 [n_seqs], row_starts int32 [n_seqs + 1] or None (a row per sequence)."""
-    if pages.dim() != 2 or lengths.shape != (pages.shape[0],):
+    pages_at, shape = _flat(pages, "pages")
+    lengths_at, n_lengths = _flat(lengths, "lengths")
+    if len(shape) != 2 or n_lengths != shape[:1]:
         raise ValueError("pages must be [n_seqs, max_pages] and lengths [n_seqs]")
-    n = pages.shape[0]
-    starts = None
+    n, starts_at = shape[0], None
     if row_starts is not None:
-        if row_starts.shape != (n + 1,):
+        starts_at, n_starts = _flat(row_starts, "row_starts")
+        if n_starts != (n + 1,):
             raise ValueError("row_starts must be [n_seqs + 1]")
-        starts = _dev_ptr(row_starts, "torch.int32", "row_starts")
-    return _dev_ptr(pages, "torch.int32", "pages"), pages.shape[1], _dev_ptr(lengths, "torch.int32", "lengths"), starts, n
+    return pages_at, shape[1], lengths_at, starts_at, n
 
 
-def _cache_rows(c: GqsaCache, k, v):
-    if k.shape != v.shape or k.dim() != 3 or k.shape[1] != c.kv_heads or k.shape[2] != c.head_dim:
+def _cache_rows(c: GqsaCache, k, v, k_what: str, v_what: str):
+    """Pointers and distances of keys and values of the cache's heads, and their rows."""
+    k_at, k_row, k_head, rows, *dims = _heads(k, k_what)
+    v_at, v_row, v_head, v_rows, *v_dims = _heads(v, v_what)
+    if v_rows != rows or dims != [c.kv_heads, c.head_dim] or v_dims != dims:
         raise ValueError("keys and values must be [rows, kv_heads, head_dim] of the cache")
+    return k_at, k_row, k_head, v_at, v_row, v_head, rows
 
 
 def gqsa_cache_append(c: GqsaCache, k, v, pages, lengths, row_starts=None, stream=None) -> None:
     """New keys and values [rows, kv_heads, head_dim] become the last tokens of their sequences; lengths counts them in."""
-    _cache_rows(c, k, v)
-    _check(_lib().gqsa_cache_append(c.ptr, *_heads(k, "k"), *_heads(v, "v"), k.shape[0], *_sequences(pages, lengths, row_starts),
-                                    _stream_ptr(stream)), "gqsa_cache_append")
+    _check(_lib().gqsa_cache_append(c.ptr, *_cache_rows(c, k, v, "k", "v"), *_sequences(pages, lengths, row_starts), _stream_ptr(stream)),
+           "gqsa_cache_append")
 
 
 def gqsa_cache_read(c: GqsaCache, pages, lengths, row_starts, k_out, v_out, stream=None):
     """The values of the last tokens of each sequence, as many as it has rows in k_out and v_out [rows, kv_heads, head_dim]."""
-    _cache_rows(c, k_out, v_out)
-    _check(_lib().gqsa_cache_read(c.ptr, *_heads(k_out, "k_out"), *_heads(v_out, "v_out"), k_out.shape[0],
-                                  *_sequences(pages, lengths, row_starts), _stream_ptr(stream)), "gqsa_cache_read")
+    _check(_lib().gqsa_cache_read(c.ptr, *_cache_rows(c, k_out, v_out, "k_out", "v_out"), *_sequences(pages, lengths, row_starts),
+                                  _stream_ptr(stream)), "gqsa_cache_read")
     return k_out, v_out
 
 
 def gqsa_cache_attend(c: GqsaCache, q, pages, lengths, row_starts=None, scale: float = None, out=None, stream=None):
     """Attention of the newest rows q [rows, q_heads, head_dim] of each sequence over its cache; scale None: head_dim ** -0.5."""
-    q_at = _heads(q, "q")
-    if q.shape[2] != c.head_dim:
+    q_at, q_row, q_head, rows, heads, dim = _heads(q, "q")
+    if dim != c.head_dim:
         raise ValueError("q must be [rows, q_heads, head_dim] of the cache")
     if out is None:
         out = _like(q, stream)
-    if out.shape != q.shape:
+    out_at, out_row, out_head, *shape = _heads(out, "out")
+    if shape != [rows, heads, dim]:
         raise ValueError("out must have the shape of q")
-    _check(_lib().gqsa_cache_attend(c.ptr, *q_at, q.shape[1], q.shape[0], *_sequences(pages, lengths, row_starts),
-                                    c.head_dim ** -0.5 if scale is None else scale, *_heads(out, "out"), _stream_ptr(stream)),
+    _check(_lib().gqsa_cache_attend(c.ptr, q_at, q_row, q_head, heads, rows, *_sequences(pages, lengths, row_starts),
+                                    dim ** -0.5 if scale is None else scale, out_at, out_row, out_head, _stream_ptr(stream)),
            "gqsa_cache_attend")
     return out
 
@@ -599,18 +631,21 @@ def gqsa_cache_attend(c: GqsaCache, q, pages, lengths, row_starts=None, scale: f
 def gqsa_prompt_attend(q, k, v, q_starts, k_starts, scale: float = None, out=None, stream=None):
     """Causal attention over packed prompts: q [q_rows, q_heads, head_dim], k and v [k_rows, kv_heads, head_dim], starts int32
     [n_seqs + 1] of each sequence's rows; scale None: head_dim ** -0.5."""
-    q_at, k_at, v_at = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
-    dim = q.shape[2]
-    if k.shape != v.shape or k.shape[2] != dim:
+    q_at, q_row, q_head, rows, heads, dim = _heads(q, "q")
+    k_at, k_row, k_head, *k_shape = _heads(k, "k")
+    v_at, v_row, v_head, *v_shape = _heads(v, "v")
+    if k_shape != v_shape or k_shape[2] != dim:
         raise ValueError("k and v must be [k_rows, kv_heads, head_dim]")
-    if q_starts.dim() != 1 or q_starts.shape != k_starts.shape:
+    q_starts_at, n_starts = _flat(q_starts, "q_starts")
+    k_starts_at, shape = _flat(k_starts, "k_starts")
+    if len(n_starts) != 1 or shape != n_starts:
         raise ValueError("q_starts and k_starts must be [n_seqs + 1]")
     if out is None:
         out = _like(q, stream)
-    if out.shape != q.shape:
+    out_at, out_row, out_head, *shape = _heads(out, "out")
+    if shape != [rows, heads, dim]:
         raise ValueError("out must have the shape of q")
-    _check(_lib().gqsa_prompt_attend(*q_at, q.shape[1], q.shape[0], *k_at, *v_at, k.shape[1], k.shape[0], dim,
-                                     _dev_ptr(q_starts, "torch.int32", "q_starts"), _dev_ptr(k_starts, "torch.int32", "k_starts"),
-                                     q_starts.shape[0] - 1, dim ** -0.5 if scale is None else scale, *_heads(out, "out"),
-                                     _stream_ptr(stream)), "gqsa_prompt_attend")
+    _check(_lib().gqsa_prompt_attend(q_at, q_row, q_head, heads, rows, k_at, k_row, k_head, v_at, v_row, v_head, k_shape[1], k_shape[0], dim,
+                                     q_starts_at, k_starts_at, n_starts[0] - 1, dim ** -0.5 if scale is None else scale,
+                                     out_at, out_row, out_head, _stream_ptr(stream)), "gqsa_prompt_attend")
     return out
