@@ -485,94 +485,141 @@ struct alignas(16) AttendShared {
     int last;
 };
 
-__device__ __forceinline__ void store_partial(float* at, float a, float b)
-{
-    const uint64_t both = uint64_t{__builtin_bit_cast(uint32_t, b)} << 32 | __builtin_bit_cast(uint32_t, a);
-    __hip_atomic_store(reinterpret_cast<uint64_t*>(at), both, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
+// Partial results, which workgroups on other XCDs read: stores and loads at the agent's scope (sc1), past the caches that are not coherent, by offsets
+// in floats.  Nobody has read such a place before in the same launch, and a launch begins with empty caches.
+struct Partials {
+    __amdgpu_buffer_rsrc_t buffer;
+    static constexpr int kAgent = 16;       // sc1
 
-__device__ __forceinline__ float2 load_partial(const float* at)
-{
-    const uint64_t both = __hip_atomic_load(reinterpret_cast<const uint64_t*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return {__builtin_bit_cast(float, static_cast<uint32_t>(both)), __builtin_bit_cast(float, static_cast<uint32_t>(both >> 32))};
-}
+    __device__ __forceinline__ Partials(float* base, int floats) : buffer(__builtin_amdgcn_make_buffer_rsrc(base, 0, floats * 4, 0x00020000)) {}
+    __device__ __forceinline__ void store4(int at, float4_t v) const
+    {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), buffer, at * 4, 0, kAgent);
+    }
+    __device__ __forceinline__ void store2(int at, float a, float b) const
+    {
+        typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)}, buffer, at * 4, 0, kAgent);
+    }
+    __device__ __forceinline__ float4_t load4(int at) const
+    {
+        return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer, at * 4, 0, kAgent));
+    }
+    __device__ __forceinline__ float2 load2(int at) const
+    {
+        typedef float float2_t __attribute__((ext_vector_type(2)));
+        const float2_t v = __builtin_bit_cast(float2_t, __builtin_amdgcn_raw_buffer_load_b64(buffer, at * 4, 0, kAgent));
+        return {v[0], v[1]};
+    }
+};
 
 constexpr int kHeld = 2;             // tiles that a wavefront holds: the one at work, and those under way
 constexpr int kAttendWaves = 4;      // wavefronts of a workgroup; a step: one tile for each
 
-// Joins `parts` partial results of `rows` rows in their order -- part_of(p): maximum, sum, weighted sum -- and hands each four elements of a row to `sink`.  With few rows
-// teams of threads take every so manieth part and meet in `scratch` (LDS).  Called by a whole workgroup.
-template <int D, int THREADS, typename PartOf, typename Sink>
-__device__ __forceinline__ void join(int rows, int parts, float* scratch, PartOf part_of, Sink sink)
+constexpr int kFan = 16;        // parts that one workgroup joins alone
+
+// Joins `parts` (up to kFan) partial results of `rows` rows in their order -- place(p): where part p lies -- and hands each four elements of a row to
+// `sink`.  All loads are under way together (or kAhead parts' at a time), or each round of them would cost the latency of memory anew.
+// Called by a whole workgroup; `scratch` is LDS for 2 kFan ROWS floats.
+template <int D, int ROWS, int THREADS, typename Place, typename Sink>
+__device__ __forceinline__ void join(const Partials& partials, int rows, int parts, float* scratch, Place place, Sink sink)
 {
-    constexpr int kAhead = 4;       // parts whose loads are under way together
-    const int columns = rows * (D / 4), teams = max(1, THREADS / columns);
-    for (int i = threadIdx.x; i < columns * teams; i += THREADS) {
-        const int team = teams == 1 ? 0 : i / columns, of = i - team * columns, r = of / (D / 4), column = 4 * (of % (D / 4));
-        float top = kMinusInf, s = 0.0f;
-        float4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int p0 = team; p0 < parts; p0 += teams * kAhead) {
-            float2 x[kAhead], y[kAhead], z[kAhead];
+    constexpr int kSets = (ROWS * (D / 4) + THREADS - 1) / THREADS;      // fours of elements per thread
+    constexpr int kAhead = 32 / kSets < kFan ? 32 / kSets : kFan;
+    float4_t x[kAhead][kSets];
+    const auto load = [&](int p0) {
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const float* part = part_of(min(p0 + j * teams, parts - 1));
-                x[j] = load_partial(part + r * D + column);
-                y[j] = load_partial(part + r * D + column + 2);
-                z[j] = load_partial(part + kRowBlock * D + 2 * r);
-            }
+        for (int j = 0; j < kAhead; ++j) {
+            if (p0 + j >= parts) break;
+            const int from = place(p0 + j);
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                if (p0 + j * teams >= parts) break;
-                const float both = fmaxf(top, z[j].x);
-                const float f = weight_of(top, both), g = weight_of(z[j].x, both);
-                s = f * s + g * z[j].y;
-                v = f * v + g * float4_t{x[j].x, x[j].y, y[j].x, y[j].y};
-                top = both;
-            }
+            for (int k = 0; k < kSets; ++k) x[j][k] = partials.load4(from + min(static_cast<int>(threadIdx.x) + k * THREADS, rows * (D / 4) - 1) * 4);
         }
-        if (teams == 1) {
-            sink(r, column, v, top, s);
-        } else {
-            float* at = scratch + i * 6;
-            at[0] = top, at[1] = s, at[2] = v[0], at[3] = v[1], at[4] = v[2], at[5] = v[3];
+    };
+    load(0);
+    float* weights = scratch;               // [part][row]: maximum, then weight
+    float* sums = scratch + kFan * ROWS;
+    for (int i = threadIdx.x; i < parts * rows; i += THREADS) {
+        const int part = i / rows, r = i - part * rows;
+        const float2 top_sum = partials.load2(place(part) + ROWS * D + 2 * r);
+        weights[part * ROWS + r] = top_sum.x, sums[part * ROWS + r] = top_sum.y;
+    }
+    __syncthreads();
+    float mine[(kFan * ROWS + THREADS - 1) / THREADS];
+#pragma unroll
+    for (int k = 0; k < (kFan * ROWS + THREADS - 1) / THREADS; ++k) {
+        const int i = threadIdx.x + k * THREADS;
+        if (i >= parts * rows) break;
+        const int part = i / rows, r = i - part * rows;
+        float top = kMinusInf;
+        for (int q = 0; q < parts; ++q) top = fmaxf(top, weights[q * ROWS + r]);
+        mine[k] = weight_of(weights[part * ROWS + r], top);
+        if (part == 0) sums[kFan * ROWS + r] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < (kFan * ROWS + THREADS - 1) / THREADS; ++k) {
+        const int i = threadIdx.x + k * THREADS;
+        if (i >= parts * rows) break;
+        const int part = i / rows, r = i - part * rows;
+        weights[part * ROWS + r] = mine[k];
+    }
+    __syncthreads();
+    float4_t v[kSets];
+    float s[kSets];
+#pragma unroll
+    for (int k = 0; k < kSets; ++k) v[k] = float4_t{0.0f, 0.0f, 0.0f, 0.0f}, s[k] = 0.0f;
+    for (int p0 = 0; p0 < parts; p0 += kAhead) {
+        if (p0 > 0) load(p0);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (p0 + j >= parts) break;
+#pragma unroll
+            for (int k = 0; k < kSets; ++k) {
+                const int r = min(static_cast<int>(threadIdx.x + k * THREADS) / (D / 4), rows - 1);
+                const float w = weights[(p0 + j) * ROWS + r];
+                s[k] += w * sums[(p0 + j) * ROWS + r];
+                v[k] += w * x[j][k];
+            }
         }
     }
-    if (teams == 1) return;
-    __syncthreads();
-    for (int of = threadIdx.x; of < columns; of += THREADS) {
-        float top = kMinusInf;
-        for (int k = 0; k < teams; ++k) top = fmaxf(top, scratch[(k * columns + of) * 6]);
-        float s = 0.0f;
-        float4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int k = 0; k < teams; ++k) {
-            const float* p = scratch + (k * columns + of) * 6;
-            const float f = weight_of(p[0], top);
-            s += f * p[1];
-            v += f * float4_t{p[2], p[3], p[4], p[5]};
-        }
-        sink(of / (D / 4), 4 * (of % (D / 4)), v, top, s);
+#pragma unroll
+    for (int k = 0; k < kSets; ++k) {
+        const int of = threadIdx.x + k * THREADS;
+        if (of < rows * (D / 4)) sink(of / (D / 4), 4 * (of % (D / 4)), v[k], sums[kFan * ROWS + of / (D / 4)], s[k]);
     }
     __syncthreads();       // (`scratch` is free again)
 }
 
-constexpr int kFan = 16;        // parts that one workgroup joins alone
+__device__ __forceinline__ int steps_of(const Sequence& q, int step_tiles)
+{
+    return max(static_cast<int>(static_cast<unsigned>(q.length + step_tiles * kTileTokens - 1) / static_cast<unsigned>(step_tiles * kTileTokens)), 1);
+}
 
-// The work is dealt by steps of 128 tokens, not by sequences or heads: of all steps, in the order sequence, head, block of 16 rows, token, every
+constexpr unsigned kFewSteps = 2;
+
+// The work is dealt by steps of 128 or 256 tokens, not by sequences or heads: of all steps, in the order sequence, head, block of 16 rows, token, every
 // workgroup takes a run, all of one length or one more.  Where a segment (one block of rows of one head) lies in several workgroups, each
 // leaves its maximum, sum and weighted sum in the workspace, and the last to arrive joins them in the order of the tokens.
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
 {
-    constexpr int kThreads = 64 * WAVES, kStepTiles = WAVES;
+    constexpr int kThreads = 64 * WAVES;
     constexpr int kPartial = kRowBlock * (D + 2);
     __shared__ AttendShared<D, WAVES> shared;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), quad = lane >> 4;
     const unsigned per = a.heads_per_group;
+    const Partials partials(a.partials, 3 * kAttendWorkgroups * kPartial);
     const auto blocks_of = [&](const Sequence& q) { return static_cast<int>((static_cast<unsigned>(q.rows) * per + kRowBlock - 1) / kRowBlock); };
-    const auto steps_of = [](const Sequence& q) { return max((q.length + kStepTiles * kTileTokens - 1) / (kStepTiles * kTileTokens), 1); };
-    const auto deal = deal_out<Sequence>(a.seqs.n_seqs, lane, [&](int b) { return sequence(a.seqs, a.pool.page_shift, b); }, [&](const Sequence& q) {
-        return static_cast<unsigned>(min(static_cast<int64_t>(blocks_of(q)) * steps_of(q) * a.pool.kv_heads, int64_t{INT_MAX}));
+    // A step is one tile for every wavefront; or two, where there are so few that a workgroup has one or two of them: half the parts to join.
+    int step_tiles = WAVES;
+    auto deal = deal_out<Sequence>(a.seqs.n_seqs, lane, [&](int b) { return sequence(a.seqs, a.pool.page_shift, b); }, [&](const Sequence& q) {
+        return static_cast<unsigned>(min(static_cast<int64_t>(blocks_of(q)) * steps_of(q, step_tiles) * a.pool.kv_heads, int64_t{INT_MAX}));
     });
+    if (deal.total <= kFewSteps * gridDim.x) {
+        step_tiles = 2 * WAVES;
+        deal.recount();
+    }
     const unsigned total = deal.total, workers = min(gridDim.x, total), me = blockIdx.x;
     if (me >= workers) return;
     const unsigned share = total / workers, more = total - share * workers;      // the first `more` workgroups take one step more
@@ -586,7 +633,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
     int b, within;
     Sequence seq = deal.locate(at, &b, &within);
     while (at < end) {
-        const int blocks = blocks_of(seq), steps = steps_of(seq);
+        const int blocks = blocks_of(seq), steps = steps_of(seq, step_tiles);
         if (within >= blocks * steps * a.pool.kv_heads) {       // (on to the next sequence that has rows)
             within = 0;
             seq = sequence(a.seqs, a.pool.page_shift, ++b);
@@ -614,7 +661,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
             if (a.negate) q[g] = -q[g];
         }
         const int least = before + token0 + 1, most = before + token0 + (head0 + rows - 1) / per + 1;    // tokens that the block's first and last row see
-        const int tiles = uniform(min((max(most, 0) + kTileTokens - 1) / kTileTokens, to * kStepTiles));
+        const int tiles = uniform(min((max(most, 0) + kTileTokens - 1) / kTileTokens, to * step_tiles));
 
         RowState<D> state;
         state.top = kMinusInf;
@@ -622,18 +669,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) state.out[c] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-        // The wavefront's tiles are every kStepTiles-th one; lane i knows the page of the i-th of the next 64, so that no load waits for another.
+        // The wavefront's tiles are every WAVES-th one; lane i knows the page of the i-th of the next 64, so that no load waits for another.
         const int32_t* table = a.seqs.pages + int64_t{b} * a.seqs.max_pages;
-        const int first_tile = uniform(from * kStepTiles + wave), count = max(tiles - first_tile + kStepTiles - 1, 0) / kStepTiles;
+        const int first_tile = uniform(from * step_tiles + wave), count = max(tiles - first_tile + WAVES - 1, 0) / WAVES;
         int page_of_lane = 0;
         // (always the same number of loads, past the end and for absent pages of some tile that is there: where loads are sometimes left out, the
         // compiler cannot tell those of the tile at work from those under way, and waits for all)
         const auto load = [&](int i, Raw<D>& raw) {
             const int of = min(i, count - 1);
-            if ((i & 63) == 0 && i < count) page_of_lane = opaque(table[min(first_tile + (i + lane) * kStepTiles, tiles - 1) >> (a.pool.page_shift - 5)]);
+            if ((i & 63) == 0 && i < count) page_of_lane = opaque(table[min(first_tile + (i + lane) * WAVES, tiles - 1) >> (a.pool.page_shift - 5)]);
             const int page = __builtin_amdgcn_readlane(page_of_lane, of & 63);
             const bool there = page >= 0 && page < a.pool.n_pages;
-            const int t = first_tile + of * kStepTiles;
+            const int t = first_tile + of * WAVES;
             raw.first_token = there && i < count ? t * kTileTokens : -1;
             const uint8_t* tile = a.pool.tile<D>(there ? page : 0, head, t);
 #pragma unroll
@@ -680,12 +727,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
             for (int i = 0; i < 4; ++i) y[i] = s == 0.0f ? static_cast<_Float16>(0.0f) : static_cast<_Float16>(v[i] / s);
             *reinterpret_cast<half4_t*>(a.out.data + int64_t{seq.start + static_cast<int>(token0 + on)} * a.out.row + to_head * a.out.head + column) = y;
         };
-        const auto put = [&](float* part, int r, int column, float4_t v, float top, float s) {
-            store_partial(part + r * D + column, v[0], v[1]);
-            store_partial(part + r * D + column + 2, v[2], v[3]);
-            if (column == 0) store_partial(part + kRowBlock * D + 2 * r, top, s);
+        const auto put = [&](int part, int r, int column, float4_t v, float top, float s) {
+            partials.store4(part + r * D + column, v);
+            if (column == 0) partials.store2(part + kRowBlock * D + 2 * r, top, s);
         };
-        float* partial = a.partials + (2 * me + (from == 0 ? 1 : 0)) * kPartial;
+        const int partial = (2 * me + (from == 0 ? 1 : 0)) * kPartial;
         for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
             const int r = i / (D / 4), column = 4 * (i % (D / 4));
             float top = shared.top[0][r];
@@ -708,8 +754,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
             // workgroup would read all parts alone (of 64 parts of 8 rows 262 KB).
             const unsigned segment_start = at - from, w0 = owner_of(segment_start);
             const int parts = owner_of(segment_start + steps - 1) - w0 + 1, mine = me - w0;
-            // Parts are written and read by agent-scope atomic operations, which pass the caches that are not coherent, and the counters count them only when they have
-            // arrived.  (A release and an acquire around the counters would write back and empty whole L2 caches: 3 times the kernel's time.)
+            // The counters count a part only when all its stores have arrived.  (A release and an acquire around the counters would write back and empty whole L2 caches: 3 times the kernel's time.)
             const auto arrived_last = [&](int* counter, int all) {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
@@ -720,17 +765,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
                 __syncthreads();
                 return shared.last != 0;
             };
-            const auto part_of = [&](int p) { return a.partials + (2 * (w0 + p) + (p == 0 ? 1 : 0)) * kPartial; };
-            const auto joint_of = [&](int g) { return a.partials + (2 * kAttendWorkgroups + w0 + g * kFan) * kPartial; };
+            const auto part_of = [&](int p) { return static_cast<int>(2 * (w0 + p) + (p == 0 ? 1 : 0)) * kPartial; };
+            const auto joint_of = [&](int g) { return static_cast<int>(2 * kAttendWorkgroups + w0 + g * kFan) * kPartial; };
             const auto finish = [&](int r, int column, float4_t v, float, float s) { write(r, column, v, s); };
             if (parts <= kFan) {
-                if (arrived_last(a.arrivals + w0, parts)) join<D, kThreads>(rows, parts, &shared.out[0][0][0], part_of, finish);
+                if (arrived_last(a.arrivals + w0, parts)) join<D, kRowBlock, kThreads>(partials, rows, parts, &shared.out[0][0][0], part_of, finish);
             } else {
                 const int g = mine / kFan, groups = (parts + kFan - 1) / kFan;
                 if (arrived_last(a.arrivals + w0 + g * kFan, min(kFan, parts - g * kFan))) {
-                    join<D, kThreads>(rows, min(kFan, parts - g * kFan), &shared.out[0][0][0], [&](int p) { return part_of(g * kFan + p); },
+                    join<D, kRowBlock, kThreads>(partials, rows, min(kFan, parts - g * kFan), &shared.out[0][0][0], [&](int p) { return part_of(g * kFan + p); },
                                       [&](int r, int column, float4_t v, float top, float s) { put(joint_of(g), r, column, v, top, s); });
-                    if (arrived_last(a.arrivals + kAttendWorkgroups + w0, groups)) join<D, kThreads>(rows, groups, &shared.out[0][0][0], joint_of, finish);
+                    if (arrived_last(a.arrivals + kAttendWorkgroups + w0, groups)) join<D, kRowBlock, kThreads>(partials, rows, groups, &shared.out[0][0][0], joint_of, finish);
                 }
             }
         }
@@ -823,8 +868,9 @@ gqsa_status_t cache_attend(gqsa_cache* c, const Heads& q, int q_heads, const Seq
     if (steps > INT_MAX) return GQSA_ERR_SHAPE;
     const unsigned grid = static_cast<unsigned>(std::max(1.0, std::min<double>(kAttendWorkgroups, steps)));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (c->head_dim == 128) hipLaunchKernelGGL((attend_kernel<128, kAttendWaves>), dim3(grid), dim3(64 * kAttendWaves), 0, s, a);
-    else hipLaunchKernelGGL((attend_kernel<64, kAttendWaves>), dim3(grid), dim3(64 * kAttendWaves), 0, s, a);
+    const dim3 threads(64 * kAttendWaves);
+    if (c->head_dim == 128) hipLaunchKernelGGL((attend_kernel<128, kAttendWaves>), dim3(grid), threads, 0, s, a);
+    else hipLaunchKernelGGL((attend_kernel<64, kAttendWaves>), dim3(grid), threads, 0, s, a);
     GQSA_HIP(hipGetLastError());
     return GQSA_OK;
 }

@@ -49,6 +49,12 @@ struct Deal {
     __device__ __forceinline__ Deal(int n_seqs_, int lane_, Load load_, Count count_) : n_seqs(n_seqs_), lane(lane_), load(load_), count(count_)
     {
         seq = load(min(lane, n_seqs - 1));
+        recount();
+    }
+
+    // (again, where count() has changed)
+    __device__ __forceinline__ void recount()
+    {
         own = lane < n_seqs ? count(seq) : 0u;
         upto = running_sum(own);
         total = of_first = last(upto);

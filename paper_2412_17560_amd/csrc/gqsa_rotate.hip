@@ -120,9 +120,10 @@ void launch(const RotateCall& c, hipStream_t s)
 {
     constexpr int kHeadsAtOnce = 64 / LANES;
     const int sets = (c.q_heads + c.k_heads + kHeadsAtOnce - 1) / kHeadsAtOnce;
-    // One wavefront per row keeps the row's part of the table in registers; with fewer rows than fill the chip (8 wavefronts a
-    // SIMD) the sets of heads of a row are spread.
-    const int waves_per_row = static_cast<int>(std::min<int64_t>(sets, std::max<int64_t>(1, 8192 / c.n_rows)));
+    // A wavefront keeps its row's part of the table in registers over all the heads it takes, so few to a row read it less often; but there should be some
+    // four times as many as the chip holds at once (7 a SIMD), or the last of them run alone: 8192 rows of 72 heads of 128 take 73.6 us with
+    // 8192 wavefronts, 66.0, 63.1 and 62.6 with 16384, 32768 and all of one set of heads each; 16384 rows of 40 heads of 64 41.9, 41.6, 39.5, 41.0.
+    const int waves_per_row = static_cast<int>(std::min<int64_t>(sets, std::max<int64_t>(1, 32768 / c.n_rows)));
     const int64_t waves = c.n_rows * waves_per_row;
     const dim3 grid(static_cast<unsigned>((waves + kThreads / 64 - 1) / (kThreads / 64)));
     if (c.interleaved) hipLaunchKernelGGL((rotate_kernel<LANES, true>), grid, dim3(kThreads), 0, s, c, waves_per_row);
