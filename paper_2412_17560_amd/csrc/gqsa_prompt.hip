@@ -16,8 +16,8 @@ namespace gqsa {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBlockRows = 128;     // query rows of a workgroup
-constexpr int kWaveRows = 32;
+constexpr int kWaves = kThreads / 64;
+constexpr int kWaveRows = 32;       // query rows of a wavefront
 constexpr int kTileKeys = 64;
 constexpr float kSlack = 8.0f;      // powers of two that a score may lie above its row's reference before the reference follows
 
@@ -72,14 +72,18 @@ __device__ __forceinline__ bool some_not_finite(const uint16_t* tile)
     return (over & 0x80008000u) != 0;
 }
 
-template <int D>
+// SPLIT: how many wavefronts share their rows, each with every SPLIT-th part of a tile's keys.  With 2 a workgroup has 64 rows instead of 128.
+template <int D, int SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool negate)
 {
+    constexpr int kGroups = kWaves / SPLIT, kBlockRows = kGroups * kWaveRows;
+    constexpr int kPieces = 2 / SPLIT;               // runs of 32 keys of a tile that a wavefront takes
     constexpr int kCopies = D / 32;                  // KiB of a tile of keys that a wavefront copies
     constexpr int kCopyRows = 512 / D;               // rows in one of them
     constexpr int kLanesPerRow = D / 8;
     __shared__ PromptShared<D> shared;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5;
+    const int group = wave % kGroups, part = wave / kGroups;
 
     struct Prompt {
         int start, rows, length;       // query rows, and where they start; keys
@@ -98,7 +102,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
     const Prompt prompt = deal.locate(deal.total - 1 - slot, &b, &block);
     const int q_start = prompt.start, n_q = prompt.rows, n_k = prompt.length, k_start = start_of(c.k_starts, c.n_k_rows, b);
     const int behind = n_k - n_q;                    // row r sees keys 0 .. r + behind
-    const int row0 = block * kBlockRows, wave_row0 = row0 + wave * kWaveRows;
+    const int row0 = block * kBlockRows, wave_row0 = row0 + group * kWaveRows;
     const int row = wave_row0 + (lane & 31);
     const int sees = row + behind + 1;
     const int keys = max(min(n_q, row0 + kBlockRows) + behind, 0);                               // that some row of the block sees
@@ -142,22 +146,23 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wavefront's part of the tile has arrived,
         __syncthreads();                                       // everybody's has, and nobody reads the other buffer any more
         if (tile + 1 < tiles) copy(tile + 1, buffer ^ 1);
-        const bool active = first < wave_keys;                 // (the same for a whole wavefront)
+        const int mine = first + 32 * kPieces * part;          // this wavefront's first key
+        const bool active = mine < wave_keys;                 // (the same for a whole wavefront)
         const uint16_t *k_tile = shared.k[buffer], *v_tile = shared.v[buffer];
         // The two (with keys of an earlier part three) tiles that some rows see in part.  If values there are not finite, the rows that do not see them must
         // be kept from them: see below.
         bool wild = false;
         if (first + kTileKeys > row0 + behind + 1) wild = __syncthreads_or(some_not_finite<D>(v_tile));
 
-        float16_t s[2];
+        float16_t s[kPieces];
         if (active) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) s[j] = float16_t{};
+            for (int j = 0; j < kPieces; ++j) s[j] = float16_t{};
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = 32 * j + (lane & 31);
+                for (int j = 0; j < kPieces; ++j) {
+                    const int r = 32 * (kPieces * part + j) + (lane & 31);
                     const half8_t k = *reinterpret_cast<const half8_t*>(k_tile + r * D + 8 * key_place<D>(r, 2 * i + half));
                     s[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i], s[j], 0, 0, 0);
                 }
@@ -176,17 +181,17 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
             __syncthreads();
         }
         if (!active) continue;
-        // element r of s[j] is key 32 j + r % 4 + 8 (r / 4) + 4 half
-        if (first + kTileKeys > wave_row0 + behind + 1) {
+        // element r of s[j] is key 32 j + r % 4 + 8 (r / 4) + 4 half of the wavefront's
+        if (mine + 32 * kPieces > wave_row0 + behind + 1) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kPieces; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (first + 32 * j + (r & 3) + 8 * (r >> 2) + 4 * half >= sees) s[j][r] = kMinusInf;
+                    if (mine + 32 * j + (r & 3) + 8 * (r >> 2) + 4 * half >= sees) s[j][r] = kMinusInf;
         }
         float most = kMinusInf;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < kPieces; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[j][r]);
         most *= c.scale;
@@ -200,15 +205,20 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
             for (int i = 0; i < D / 32; ++i) out[i] *= shrink;
         }
         const float reference = top == kMinusInf ? 0.0f : top;
-        half8_t p[4];
+        half8_t p[2 * kPieces];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2 * kPieces; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + e], c.scale, -reference));
-                sum += x;
-                p[i][e] = static_cast<_Float16>(x);
+                p[i][e] = static_cast<_Float16>(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + e], c.scale, -reference)));
             }
+        // (the sum of the weights as the product has them, rounded: half the additions)
+        const half2_t ones = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
+#pragma unroll
+        for (int i = 0; i < 2 * kPieces; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2(half2_t{p[i][e], p[i][e + 1]}, ones, sum, false);
+        __builtin_amdgcn_s_setprio(1);      // (products ahead of the other wavefronts' softmax: 2 %)
         // The operand V^T: 16 lanes read 4 keys x 16 elements, each 4 elements of a key, and get 4 keys of an element each.
         const auto turned = [&](const uint16_t* tile, int i, int d) {
             short4_t part[2];
@@ -221,19 +231,20 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
             return __builtin_shufflevector(__builtin_bit_cast(half4_t, part[0]), __builtin_bit_cast(half4_t, part[1]), 0, 1, 2, 3, 4, 5, 6, 7);
         };
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2 * kPieces; ++i)
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(turned(v_tile, i, d), p[i], out[d], 0, 0, 0);
+            for (int d = 0; d < D / 32; ++d) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(turned(v_tile, 2 * kPieces * part + i, d), p[i], out[d], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
         if (wild) {
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) {
                 float16_t count = float16_t{};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < 2 * kPieces; ++i) {
                     half8_t seen;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) seen[e] = static_cast<_Float16>(first + 16 * i + 8 * (e >> 2) + 4 * half + (e & 3) < sees ? 1.0f : 0.0f);
-                    count = __builtin_amdgcn_mfma_f32_32x32x16_f16(turned(k_tile, i, d), seen, count, 0, 0, 0);
+                    for (int e = 0; e < 8; ++e) seen[e] = static_cast<_Float16>(mine + 16 * i + 8 * (e >> 2) + 4 * half + (e & 3) < sees ? 1.0f : 0.0f);
+                    count = __builtin_amdgcn_mfma_f32_32x32x16_f16(turned(k_tile, 2 * kPieces * part + i, d), seen, count, 0, 0, 0);
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) out[d][r] += from_counts(count[r]);
@@ -243,6 +254,27 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
     }
 
     sum += __shfl_xor(sum, 32);
+    if constexpr (SPLIT > 1) {
+        // the other part of the keys, by way of LDS
+        float* meet = reinterpret_cast<float*>(&shared) + group * (16 * (D / 32) + 2) * 64 + lane;
+        __syncthreads();
+        if (part == 1) {
+            meet[0] = top, meet[64] = sum;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) meet[(2 + 16 * d + r) * 64] = out[d][r];
+        }
+        __syncthreads();
+        if (part == 1) return;
+        const float other = meet[0], both = fmaxf(top, other);
+        const float f = top == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(top - both), g = other == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(other - both);
+        sum = f * sum + g * meet[64];
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) out[d][r] = f * out[d][r] + g * meet[(2 + 16 * d + r) * 64];
+    }
     if (row >= n_q) return;
     uint16_t* to = c.out.data + (int64_t{q_start} + row) * c.out.row + head * c.out.head + 4 * half;
 #pragma unroll
@@ -264,12 +296,27 @@ gqsa_status_t prompt_attend(const PromptCall& call, void* stream)
     const bool negate = c.scale < 0.0f;     // of the queries instead: the largest score is then the one of the largest product
     // (the softmax is taken to base 2; not 0, so that a masked score stays -infinity: 1e-30 leaves every weight at 1)
     c.scale = std::max(std::fabs(c.scale) * 1.44269504088896341f, 1e-30f);
-    const int64_t blocks = (c.n_q_rows / kBlockRows + c.n_seqs) * c.q_heads;      // no fewer than there are
+    // Few workgroups: rows shared by two wavefronts, so that there are twice as many.  us of own / shared rows, heads of 128, by the workgroups of 128 rows
+    // (bound below):
+    //   keys of 1000 and more: 128 rows 1 x 128 + 2000 keys x 32 heads 46.9 / 35.0; 160: 512 + 2000 keys 59.7 / 44.2; 224: 2000 x 14 heads 52.5 / 39.3; 352: 1300 x 32
+    //     38.4 / 34.2; 384: 1500 x 32 43.4 / 39.5; 448: 4000 x 14 100 / 89.5; 576: 1024 x 64 35.7 / 40.0;
+    //   fewer: 96: 256 x 32 12.5 / 11.5; 192: 700 x 32 21.6 / 19.4; 320: 4 x 194 x 32 14.9 / 14.1, 8 x 100 x 32 (352) 10.5 / 11.8; 384: 700 x 64 25.5 / 28.2;
+    //     392: 2 x 800 x 28 28.7 / 30.0; one tile of keys (15 x 32) 7.8 / 8.4, 16 x 64 x 14 8.1 / 9.2.
+    // (Four tiles in LDS instead of two, where every workgroup has a compute unit for itself, took 1.1 to 1.25 times as long.)
+    const auto blocks_of = [&](int rows) { return (c.n_q_rows / rows + c.n_seqs) * c.q_heads; };      // no fewer than there are
+    const int64_t whole = blocks_of(kWaves * kWaveRows), half = blocks_of(kWaves * kWaveRows / 2);
+    const bool split = c.n_k_rows > kTileKeys * int64_t{c.n_seqs} && whole <= (c.n_k_rows >= int64_t{1000} * c.n_seqs ? 512 : 256);
+    const int64_t blocks = split ? half : whole;
     if (blocks > (int64_t{1} << 23)) return GQSA_ERR_SHAPE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid(static_cast<unsigned>(blocks));
-    if (c.head_dim == 128) hipLaunchKernelGGL(prompt_kernel<128>, grid, dim3(kThreads), 0, s, c, negate);
-    else hipLaunchKernelGGL(prompt_kernel<64>, grid, dim3(kThreads), 0, s, c, negate);
+    if (c.head_dim == 128) {
+        if (split) hipLaunchKernelGGL((prompt_kernel<128, 2>), grid, dim3(kThreads), 0, s, c, negate);
+        else hipLaunchKernelGGL((prompt_kernel<128, 1>), grid, dim3(kThreads), 0, s, c, negate);
+    } else {
+        if (split) hipLaunchKernelGGL((prompt_kernel<64, 2>), grid, dim3(kThreads), 0, s, c, negate);
+        else hipLaunchKernelGGL((prompt_kernel<64, 1>), grid, dim3(kThreads), 0, s, c, negate);
+    }
     GQSA_HIP(hipGetLastError());
     return GQSA_OK;
 }
