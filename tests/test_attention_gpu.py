@@ -548,3 +548,71 @@ def test_the_binding_refuses():
                  lambda: gq.gqsa_qk_norm_rotate(x, None, None, None, x[0, 0, :32])):
         with pytest.raises(ValueError):
             call()
+
+
+# ----------------------------------------------------------------------------- all of it together
+def test_layer_of_prompts_and_steps():
+    """Products, norms, rotation, cache and attention as a decoder layer runs them: every stage against the definition, from the stage's own inputs."""
+    import gqsa_inputs as gi
+    import oracle
+    from paper_2412_17560_amd.attention_layer import AttentionLayer, rotary_table
+
+    hidden, heads, kv_heads, dim, counts = 256, 4, 2, 64, [37, 5]
+    sizes = [(heads * dim, hidden), (kv_heads * dim, hidden), (kv_heads * dim, hidden), (hidden, heads * dim)]
+    weights = [gi.dense_weight(n, k, seed=i) for i, (n, k) in enumerate(sizes)]
+    packed = [oracle.pack(w, 16, 4, sparsity=0.5) for w in weights]
+    c = Cached([0, 0], kv_heads, dim, 32, room=64)
+    norms = [dev(normal(c.rng, dim)) for _ in range(2)]
+    table = rotary_table(64, dim)
+    layer = AttentionLayer(*[gq.gqsa_pack(w, 16, 4, 0.5) for w in weights], heads, table, c.cache, *norms)
+    seen = {}
+
+    def watch(name, original):
+        def call(*args, **kw):
+            inputs = [a.cpu().numpy().copy() if torch.is_tensor(a) else a for a in args]
+            out = original(*args, **kw)
+            seen[name] = inputs, out
+            return out
+        return call
+
+    starts = np.cumsum([0] + counts).astype(np.int32)
+    positions = np.concatenate([np.arange(n) for n in counts]).astype(np.int32)
+    with pytest.MonkeyPatch.context() as m:
+        for name in ("gqsa_qk_norm_rotate", "gqsa_cache_append", "gqsa_prompt_attend", "gqsa_cache_attend"):
+            m.setattr(gq, name, watch(name, getattr(gq, name)))
+        x = normal(c.rng, sum(counts), hidden)
+        y = layer.prompt(dev(x), dev(positions), dev(c.pages), dev(starts), ints(*counts))
+        prompt_seen = dict(seen)
+        row = normal(c.rng, 2, hidden)
+        z = layer.step(dev(row), ints(*counts), dev(c.pages), ints(*(n + 1 for n in counts)))
+
+    def product(p, a):
+        return np.stack([r for r in oracle.gemv(p, a)])
+
+    for seen_now, rows, where in ((prompt_seen, x, positions), (seen, row, np.array(counts))):
+        q, k = seen_now["gqsa_qk_norm_rotate"][0][:2]
+        for got, p in ((q, packed[0]), (k, packed[1])):
+            want = product(p, rows).reshape(got.shape)
+            assert np.abs(got - want).max() <= 2e-3 * np.abs(want).max()
+        turned = seen_now["gqsa_cache_append"][0][1]
+        _check_rotated(turned, k, positions=where, table=table.cpu().numpy(), weight=norms[1].cpu().numpy())
+    new = [(s["gqsa_cache_append"][0][1], s["gqsa_cache_append"][0][2]) for s in (prompt_seen, seen)]
+    c.k, c.v = ([np.concatenate([new[0][i][starts[b]:starts[b + 1]], new[1][i][b:b + 1]]) for b in range(2)] for i in (0, 1))
+    c.check()
+    q, k, v = prompt_seen["gqsa_prompt_attend"][0][:3]
+    attended = prompt_seen["gqsa_prompt_attend"][1].cpu().numpy()
+    _check_prompts(attended, q, k, v, starts, starts, dim ** -0.5)
+    step_q, step_out = seen["gqsa_cache_attend"][0][1], seen["gqsa_cache_attend"][1].cpu().numpy()
+    _check_cache(c, [step_q[:1], step_q[1:]], [step_out[:1], step_out[1:]])
+    for got, a in ((y, attended), (z, step_out)):
+        want = product(packed[3], a.reshape(len(a), -1))
+        assert np.abs(got.cpu().numpy() - want).max() <= 2e-3 * np.abs(want).max()
+
+
+def test_example_command(monkeypatch, capsys):
+    from paper_2412_17560_amd import attention_layer
+    monkeypatch.setattr("sys.argv", ["attention_layer", "--hidden", "512", "--heads", "8", "--kv-heads", "2", "--head-dim", "64",
+                                     "--prompts", "40,3", "--tokens", "5"])
+    attention_layer.main()
+    printed = capsys.readouterr().out
+    assert "prompts of [40, 3]: 43 rows" in printed and "4 tokens for 2 sequences" in printed
