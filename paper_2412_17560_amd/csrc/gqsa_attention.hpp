@@ -32,7 +32,7 @@ struct RotateCall {
     const int32_t* positions;
     int64_t n_rows, n_positions;
     int q_heads, k_heads, head_dim, rotary_dim, interleaved;
-    float eps;
+    float eps, one_over_dim;
 };
 
 // The tokens of a 4-bit cache are held in tiles of 32 of one head: what 16x16x32 products take (gqsa_cache.hip says in which order).

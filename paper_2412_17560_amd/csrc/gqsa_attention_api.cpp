@@ -81,6 +81,7 @@ gqsa_status_t gqsa_qk_norm_rotate(const void* q, int64_t q_row_stride, int64_t q
     c.rotary_dim = rotary_dim;
     c.interleaved = interleaved != 0;
     c.eps = eps;
+    c.one_over_dim = 1.0f / static_cast<float>(head_dim);
     return gqsa::rotate(c, hip_stream);
 }
 

@@ -722,9 +722,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
         const auto write = [&](int r, int column, float4_t v, float s) {
             const unsigned on = (head0 + r) / per;
             const int to_head = head * per + (head0 + r - on * per);
+            const float inverse = s == 0.0f ? 0.0f : 1.0f / s;       // (a row that sees nothing: all sums are 0)
             half4_t y;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = s == 0.0f ? static_cast<_Float16>(0.0f) : static_cast<_Float16>(v[i] / s);
+            for (int i = 0; i < 4; ++i) y[i] = static_cast<_Float16>(v[i] * inverse);
             *reinterpret_cast<half4_t*>(a.out.data + int64_t{seq.start + static_cast<int>(token0 + on)} * a.out.row + to_head * a.out.head + column) = y;
         };
         const auto put = [&](int part, int r, int column, float4_t v, float top, float s) {

@@ -276,6 +276,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
             for (int r = 0; r < 16; ++r) out[d][r] = f * out[d][r] + g * meet[(2 + 16 * d + r) * 64];
     }
     if (row >= n_q) return;
+    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;       // (a row without keys: all sums are 0)
     uint16_t* to = c.out.data + (int64_t{q_start} + row) * c.out.row + head * c.out.head + 4 * half;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -283,7 +284,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
         for (int r = 0; r < 4; ++r) {
             half4_t y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = sum == 0.0f ? static_cast<_Float16>(0.0f) : static_cast<_Float16>(out[d][4 * r + e] / sum);
+            for (int e = 0; e < 4; ++e) y[e] = static_cast<_Float16>(out[d][4 * r + e] * inverse);
             *reinterpret_cast<half4_t*>(to + 32 * d + 8 * r) = y;
         }
 }

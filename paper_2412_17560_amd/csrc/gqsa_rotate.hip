@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateCall c, int wave
         for (int m = 1; m < LANES; m *= 2) sum += __shfl_xor(sum, m);
         if (!held || head >= heads) continue;
         if (weight) {
-            const float r = rsqrtf(sum / static_cast<float>(c.head_dim) + c.eps);
+            const float r = rsqrtf(__builtin_fmaf(sum, c.one_over_dim, c.eps));
             const half8_t wa = *reinterpret_cast<const half8_t*>(weight + 8 * run_a);
             const half8_t wb = *reinterpret_cast<const half8_t*>(weight + 8 * run_b);
 #pragma unroll
