@@ -318,11 +318,21 @@ def _shape(h: GqsaHandle):
     return h.shape
 
 
+_TORCH = None
+
+
+def _torch():
+    global _TORCH
+    import torch
+    _TORCH = torch
+    return torch
+
+
 def _stream_ptr(stream):
     if stream is None:
-        import torch
-        try:                 # (not a public name, but torch.cuda.current_stream() makes an object a call)
-            return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        torch = _TORCH or _torch()
+        try:                 # (not public names, but torch.cuda.current_stream() makes an object a call)
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         except AttributeError:
             return torch.cuda.current_stream().cuda_stream
     return C.c_void_p(getattr(stream, "cuda_stream", stream))      # (an integer; as an argument itself ctypes would take a text too)
@@ -455,36 +465,45 @@ def gqsa_stream_read(buf, sink, stream=None) -> None:
 # ----------------------------------------------------------------------------- between the q/k/v and the o product
 
 # These calls, too, are bound by their host work where the kernels take a few microseconds: an attribute of a tensor costs 0.05 to 0.08 us, so each
-# is asked for once (norm and rotation of one row: 11.1 us a call with the helpers above, 9.4 with these).
+# is asked for once (norm and rotation of one row: 11.1 us a call with the helpers above, 8.5 with these; 4 of them are the C call).
+
+_HALF = _INT = _FLOAT = None      # torch's dtypes, looked up by the first call
+
+
+def _names():
+    global _HALF, _INT, _FLOAT
+    import torch
+    _HALF, _INT, _FLOAT = torch.float16, torch.int32, torch.float32
+
 
 def _heads(t, what: str):
     """(pointer, distance between rows, distance between heads, rows, heads, head_dim) of a float16 device tensor [rows, heads, head_dim]
     whose heads are contiguous; the other two dimensions may be strided."""
+    if _HALF is None:
+        _names()
     try:
         rows, heads, dim = t.shape
         row, head, one = t.stride()
-        good = t.is_cuda and t.dtype is _half()
+        if one == 1 and t.dtype is _HALF and t.is_cuda:
+            # (torch lets the distance of a dimension of size 1 be anything)
+            return t.data_ptr(), row if rows > 1 else 0, head if heads > 1 else 0, rows, heads, dim
     except (AttributeError, TypeError, ValueError):
-        good, one = False, 1
-    if not good or one != 1:
-        raise ValueError(f"{what} must be a float16 device tensor [rows, heads, head_dim] with contiguous heads")
-    # (torch lets the distance of a dimension of size 1 be anything)
-    return t.data_ptr(), row if rows > 1 else 0, head if heads > 1 else 0, rows, heads, dim
+        pass
+    raise ValueError(f"{what} must be a float16 device tensor [rows, heads, head_dim] with contiguous heads")
 
 
-def _half():
-    dtype = _DTYPES.get("torch.float16")
-    if dtype is None:
-        import torch
-        dtype = _DTYPES.setdefault("torch.float16", torch.float16)
-    return dtype
+def _heads_like(t, what: str, rows: int, heads: int, dim: int):
+    """The first three of _heads, of an array of that shape."""
+    at, row, head, t_rows, t_heads, t_dim = _heads(t, what)
+    if t_rows != rows or t_heads != heads or t_dim != dim:
+        raise ValueError(f"{what} must be [{rows}, {heads}, {dim}]")
+    return at, row, head
 
 
-def _flat(t, what: str, dtype_name: str = "torch.int32"):
+def _flat(t, dtype, what: str):
     """(pointer, shape) of a contiguous device tensor of that dtype."""
-    dtype = _DTYPES.get(dtype_name)
-    if dtype is None or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        return _dev_ptr(t, dtype_name, what), t.shape         # (which says what is wrong, if anything is)
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} device tensor")
     return t.data_ptr(), t.shape
 
 
@@ -499,6 +518,13 @@ def _like(x, stream):
         return torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
+def _norm_weight(w, dim: int):
+    at, shape = _flat(w, _HALF, "norm weights")
+    if len(shape) != 1 or shape[0] != dim:
+        raise ValueError("norm weights must be [head_dim]")
+    return at
+
+
 def gqsa_qk_norm_rotate(q, k, positions, table, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
                         q_out=None, k_out=None, stream=None):
     """Norms of queries [rows, q_heads, head_dim] and keys [rows, k_heads, head_dim] per head (weights float16 [head_dim] or None: no norm)
@@ -507,39 +533,31 @@ def gqsa_qk_norm_rotate(q, k, positions, table, q_weight=None, k_weight=None, ep
     q_at, q_row, q_head, rows, q_heads, dim = _heads(q, "q")
     if q_out is None:
         q_out = _like(q, stream)
-    qo_at, qo_row, qo_head, *shape = _heads(q_out, "q_out")
-    if shape != [rows, q_heads, dim]:
-        raise ValueError("q_out must have the shape of q")
+    qo_at, qo_row, qo_head = _heads_like(q_out, "q_out", rows, q_heads, dim)
     k_at, k_row, k_head, k_heads, ko_at, ko_row, ko_head = None, 0, 0, 0, None, 0, 0
     if k is not None:
         k_at, k_row, k_head, k_rows, k_heads, k_dim = _heads(k, "k")
         if k_out is None:
             k_out = _like(k, stream)
-        ko_at, ko_row, ko_head, *shape = _heads(k_out, "k_out")
-        if k_rows != rows or k_dim != dim or shape != [rows, k_heads, dim]:
-            raise ValueError("k must be [rows, k_heads, head_dim] and k_out as k")
+        if k_rows != rows or k_dim != dim:
+            raise ValueError("k must be [rows, k_heads, head_dim]")
+        ko_at, ko_row, ko_head = _heads_like(k_out, "k_out", rows, k_heads, dim)
     n_positions = rotary = 0
     table_at = positions_at = None
     if table is not None:
-        table_at, shape = _flat(table, "table", "torch.float32")
+        table_at, shape = _flat(table, _FLOAT, "table")
         n_positions, half, two = shape if len(shape) == 3 else (0, 0, 0)
         if two != 2 or positions is None:
             raise ValueError("table must be [n_positions, rotary_dim / 2, 2] and positions [rows]")
-        positions_at, shape = _flat(positions, "positions")
-        if shape != (rows,):
+        positions_at, shape = _flat(positions, _INT, "positions")
+        if len(shape) != 1 or shape[0] != rows:
             raise ValueError("positions must be [rows]")
         rotary = 2 * half
-    weights = []
-    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        w_at = None
-        if w is not None:
-            w_at, shape = _flat(w, what, "torch.float16")
-            if shape != (dim,):
-                raise ValueError("norm weights must be [head_dim]")
-        weights.append(w_at)
+    q_weight_at = None if q_weight is None else _norm_weight(q_weight, dim)
+    k_weight_at = None if k_weight is None else _norm_weight(k_weight, dim)
     _check(_lib().gqsa_qk_norm_rotate(
-        q_at, q_row, q_head, q_heads, k_at, k_row, k_head, k_heads, rows, dim, *weights, eps, table_at, n_positions, rotary, int(interleaved),
-        positions_at, qo_at, qo_row, qo_head, ko_at, ko_row, ko_head, _stream_ptr(stream)), "gqsa_qk_norm_rotate")
+        q_at, q_row, q_head, q_heads, k_at, k_row, k_head, k_heads, rows, dim, q_weight_at, k_weight_at, eps, table_at,
+        n_positions, rotary, interleaved, positions_at, qo_at, qo_row, qo_head, ko_at, ko_row, ko_head, _stream_ptr(stream)), "gqsa_qk_norm_rotate")
     return q_out, k_out
 
 
@@ -578,24 +596,25 @@ def gqsa_cache_free(c: GqsaCache) -> None:
 
 def _sequences(pages, lengths, row_starts):
     """pages int32 [n_seqs, max_pages], lengths int32 [n_seqs], row_starts int32 [n_seqs + 1] or None (a row per sequence)."""
-    pages_at, shape = _flat(pages, "pages")
-    lengths_at, n_lengths = _flat(lengths, "lengths")
-    if len(shape) != 2 or n_lengths != shape[:1]:
+    pages_at, shape = _flat(pages, _INT, "pages")
+    lengths_at, n_lengths = _flat(lengths, _INT, "lengths")
+    if len(shape) != 2 or len(n_lengths) != 1 or n_lengths[0] != shape[0]:
         raise ValueError("pages must be [n_seqs, max_pages] and lengths [n_seqs]")
-    n, starts_at = shape[0], None
+    n, max_pages = shape
+    starts_at = None
     if row_starts is not None:
-        starts_at, n_starts = _flat(row_starts, "row_starts")
-        if n_starts != (n + 1,):
+        starts_at, shape = _flat(row_starts, _INT, "row_starts")
+        if len(shape) != 1 or shape[0] != n + 1:
             raise ValueError("row_starts must be [n_seqs + 1]")
-    return pages_at, shape[1], lengths_at, starts_at, n
+    return pages_at, max_pages, lengths_at, starts_at, n
 
 
 def _cache_rows(c: GqsaCache, k, v, k_what: str, v_what: str):
     """Pointers and distances of keys and values of the cache's heads, and their rows."""
-    k_at, k_row, k_head, rows, *dims = _heads(k, k_what)
-    v_at, v_row, v_head, v_rows, *v_dims = _heads(v, v_what)
-    if v_rows != rows or dims != [c.kv_heads, c.head_dim] or v_dims != dims:
+    k_at, k_row, k_head, rows, heads, dim = _heads(k, k_what)
+    if heads != c.kv_heads or dim != c.head_dim:
         raise ValueError("keys and values must be [rows, kv_heads, head_dim] of the cache")
+    v_at, v_row, v_head = _heads_like(v, v_what, rows, heads, dim)
     return k_at, k_row, k_head, v_at, v_row, v_head, rows
 
 
@@ -619,9 +638,7 @@ def gqsa_cache_attend(c: GqsaCache, q, pages, lengths, row_starts=None, scale: f
         raise ValueError("q must be [rows, q_heads, head_dim] of the cache")
     if out is None:
         out = _like(q, stream)
-    out_at, out_row, out_head, *shape = _heads(out, "out")
-    if shape != [rows, heads, dim]:
-        raise ValueError("out must have the shape of q")
+    out_at, out_row, out_head = _heads_like(out, "out", rows, heads, dim)
     _check(_lib().gqsa_cache_attend(c.ptr, q_at, q_row, q_head, heads, rows, *_sequences(pages, lengths, row_starts),
                                     dim ** -0.5 if scale is None else scale, out_at, out_row, out_head, _stream_ptr(stream)),
            "gqsa_cache_attend")
@@ -632,20 +649,18 @@ def gqsa_prompt_attend(q, k, v, q_starts, k_starts, scale: float = None, out=Non
     """Causal attention over packed prompts: q [q_rows, q_heads, head_dim], k and v [k_rows, kv_heads, head_dim], starts int32
     [n_seqs + 1] of each sequence's rows; scale None: head_dim ** -0.5."""
     q_at, q_row, q_head, rows, heads, dim = _heads(q, "q")
-    k_at, k_row, k_head, *k_shape = _heads(k, "k")
-    v_at, v_row, v_head, *v_shape = _heads(v, "v")
-    if k_shape != v_shape or k_shape[2] != dim:
+    k_at, k_row, k_head, k_rows, kv_heads, k_dim = _heads(k, "k")
+    if k_dim != dim:
         raise ValueError("k and v must be [k_rows, kv_heads, head_dim]")
-    q_starts_at, n_starts = _flat(q_starts, "q_starts")
-    k_starts_at, shape = _flat(k_starts, "k_starts")
+    v_at, v_row, v_head = _heads_like(v, "v", k_rows, kv_heads, dim)
+    q_starts_at, n_starts = _flat(q_starts, _INT, "q_starts")
+    k_starts_at, shape = _flat(k_starts, _INT, "k_starts")
     if len(n_starts) != 1 or shape != n_starts:
         raise ValueError("q_starts and k_starts must be [n_seqs + 1]")
     if out is None:
         out = _like(q, stream)
-    out_at, out_row, out_head, *shape = _heads(out, "out")
-    if shape != [rows, heads, dim]:
-        raise ValueError("out must have the shape of q")
-    _check(_lib().gqsa_prompt_attend(q_at, q_row, q_head, heads, rows, k_at, k_row, k_head, v_at, v_row, v_head, k_shape[1], k_shape[0], dim,
+    out_at, out_row, out_head = _heads_like(out, "out", rows, heads, dim)
+    _check(_lib().gqsa_prompt_attend(q_at, q_row, q_head, heads, rows, k_at, k_row, k_head, v_at, v_row, v_head, kv_heads, k_rows, dim,
                                      q_starts_at, k_starts_at, n_starts[0] - 1, dim ** -0.5 if scale is None else scale,
                                      out_at, out_row, out_head, _stream_ptr(stream)), "gqsa_prompt_attend")
     return out
