@@ -516,11 +516,13 @@ struct Partials {
 constexpr int kHeld = 2;             // tiles that a wavefront holds: the one at work, and those under way
 constexpr int kAttendWaves = 4;      // wavefronts of a workgroup; a step: one tile for each
 
-constexpr int kFan = 16;        // parts that one workgroup joins alone
+constexpr int kFan = 16;        // parts that one workgroup joins alone, unless they are themselves joined ones
+constexpr int kMostParts = (kAttendWorkgroups + kFan - 1) / kFan;       // of which there are up to so many
+static_assert(kMostParts >= kFan, "");
 
-// Joins `parts` (up to kFan) partial results of `rows` rows in their order -- place(p): where part p lies -- and hands each four elements of a row to
+// Joins `parts` (up to kMostParts) partial results of `rows` rows in their order -- place(p): where part p lies -- and hands each four elements of a row to
 // `sink`.  All loads are under way together (or kAhead parts' at a time), or each round of them would cost the latency of memory anew.
-// Called by a whole workgroup; `scratch` is LDS for 2 kFan ROWS floats.
+// Called by a whole workgroup; `scratch` is LDS for (2 kMostParts + 1) ROWS floats.
 template <int D, int ROWS, int THREADS, typename Place, typename Sink>
 __device__ __forceinline__ void join(const Partials& partials, int rows, int parts, float* scratch, Place place, Sink sink)
 {
@@ -538,27 +540,29 @@ __device__ __forceinline__ void join(const Partials& partials, int rows, int par
     };
     load(0);
     float* weights = scratch;               // [part][row]: maximum, then weight
-    float* sums = scratch + kFan * ROWS;
+    float* sums = scratch + kMostParts * ROWS;
+    float* tops = sums + kMostParts * ROWS;      // of all parts
     for (int i = threadIdx.x; i < parts * rows; i += THREADS) {
         const int part = i / rows, r = i - part * rows;
         const float2 top_sum = partials.load2(place(part) + ROWS * D + 2 * r);
         weights[part * ROWS + r] = top_sum.x, sums[part * ROWS + r] = top_sum.y;
     }
     __syncthreads();
-    float mine[(kFan * ROWS + THREADS - 1) / THREADS];
+    constexpr int kWeights = (kMostParts * ROWS + THREADS - 1) / THREADS;       // per thread
+    float mine[kWeights];
 #pragma unroll
-    for (int k = 0; k < (kFan * ROWS + THREADS - 1) / THREADS; ++k) {
+    for (int k = 0; k < kWeights; ++k) {
         const int i = threadIdx.x + k * THREADS;
         if (i >= parts * rows) break;
         const int part = i / rows, r = i - part * rows;
         float top = kMinusInf;
         for (int q = 0; q < parts; ++q) top = fmaxf(top, weights[q * ROWS + r]);
         mine[k] = weight_of(weights[part * ROWS + r], top);
-        if (part == 0) sums[kFan * ROWS + r] = top;
+        if (part == 0) tops[r] = top;
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < (kFan * ROWS + THREADS - 1) / THREADS; ++k) {
+    for (int k = 0; k < kWeights; ++k) {
         const int i = threadIdx.x + k * THREADS;
         if (i >= parts * rows) break;
         const int part = i / rows, r = i - part * rows;
@@ -586,7 +590,7 @@ __device__ __forceinline__ void join(const Partials& partials, int rows, int par
 #pragma unroll
     for (int k = 0; k < kSets; ++k) {
         const int of = threadIdx.x + k * THREADS;
-        if (of < rows * (D / 4)) sink(of / (D / 4), 4 * (of % (D / 4)), v[k], sums[kFan * ROWS + of / (D / 4)], s[k]);
+        if (of < rows * (D / 4)) sink(of / (D / 4), 4 * (of % (D / 4)), v[k], tops[of / (D / 4)], s[k]);
     }
     __syncthreads();       // (`scratch` is free again)
 }
@@ -607,6 +611,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
     constexpr int kThreads = 64 * WAVES;
     constexpr int kPartial = kRowBlock * (D + 2);
     __shared__ AttendShared<D, WAVES> shared;
+    static_assert(sizeof(shared.out) >= (2 * kMostParts + 1) * kRowBlock * sizeof(float), "");
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), quad = lane >> 4;
     const unsigned per = a.heads_per_group;
     const Partials partials(a.partials, 3 * kAttendWorkgroups * kPartial);
@@ -750,7 +755,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
             else put(partial, r, column, v, top, s);
         }
         if (!whole) {
-            // The first workgroup of the segment, by whose number its counters go, and how many there are.  Up to kFan parts the last workgroup to arrive joins
+            // The first workgroup of the segment, and how many there are.  Up to kFan parts the last workgroup to arrive joins
             // them; of more, every kFan neighbours are joined by the last of them to arrive, and the last of those joins the results: else one
             // workgroup would read all parts alone (of 64 parts of 8 rows 262 KB).
             const unsigned segment_start = at - from, w0 = owner_of(segment_start);
@@ -767,16 +772,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
                 return shared.last != 0;
             };
             const auto part_of = [&](int p) { return static_cast<int>(2 * (w0 + p) + (p == 0 ? 1 : 0)) * kPartial; };
-            const auto joint_of = [&](int g) { return static_cast<int>(2 * kAttendWorkgroups + w0 + g * kFan) * kPartial; };
+            // A counter and a place of a group's result go by a workgroup of the group that is not the segment's first: that one may be the last of the segment
+            // before, but no workgroup is behind the first of two segments.
+            const auto slot_of = [&](int g) { return w0 + max(g * kFan, 1); };
+            const auto joint_of = [&](int g) { return static_cast<int>(2 * kAttendWorkgroups + slot_of(g)) * kPartial; };
             const auto finish = [&](int r, int column, float4_t v, float, float s) { write(r, column, v, s); };
             if (parts <= kFan) {
-                if (arrived_last(a.arrivals + w0, parts)) join<D, kRowBlock, kThreads>(partials, rows, parts, &shared.out[0][0][0], part_of, finish);
+                if (arrived_last(a.arrivals + slot_of(0), parts)) join<D, kRowBlock, kThreads>(partials, rows, parts, &shared.out[0][0][0], part_of, finish);
             } else {
                 const int g = mine / kFan, groups = (parts + kFan - 1) / kFan;
-                if (arrived_last(a.arrivals + w0 + g * kFan, min(kFan, parts - g * kFan))) {
+                if (arrived_last(a.arrivals + slot_of(g), min(kFan, parts - g * kFan))) {
                     join<D, kRowBlock, kThreads>(partials, rows, min(kFan, parts - g * kFan), &shared.out[0][0][0], [&](int p) { return part_of(g * kFan + p); },
                                       [&](int r, int column, float4_t v, float top, float s) { put(joint_of(g), r, column, v, top, s); });
-                    if (arrived_last(a.arrivals + kAttendWorkgroups + w0, groups)) join<D, kRowBlock, kThreads>(partials, rows, groups, &shared.out[0][0][0], joint_of, finish);
+                    if (arrived_last(a.arrivals + kAttendWorkgroups + slot_of(0), groups)) join<D, kRowBlock, kThreads>(partials, rows, groups, &shared.out[0][0][0], joint_of, finish);
                 }
             }
         }

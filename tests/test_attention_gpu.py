@@ -277,6 +277,55 @@ def test_many_sequences():
     _check_cache(c, q, out)
 
 
+@pytest.mark.parametrize("kv_heads, lengths", [
+    (1, [131000]),              # one head over all workgroups
+    (1, [70001]),
+    (8, [16500]),               # heads over 65 of them, the last of which is the next one's first
+    (3, [51500]),
+    (2, [300, 68000, 900]),
+])
+def test_one_head_over_many_workgroups(kv_heads, lengths):
+    """Equal weights, which are exact, and values that rise along the sequence: a part that is missing, or counted for another, shows."""
+    c = Cached([0] * len(lengths), kv_heads, 64, 1024, seed=len(lengths), room=max(lengths))
+    k, v = [c.some(n) for n in lengths], [c.some(n) for n in lengths]
+    for x in v:
+        x += (6 * np.linspace(-1, 1, len(x))[:, None, None] * np.arange(1, kv_heads + 1)[:, None]).astype(np.float16)
+    c.append(k, v)
+    rows = [1 + b % 2 for b in range(len(lengths))]
+    for _ in range(3):                                         # (and leaves nothing behind for the next call)
+        q, out = _attend_all(c, rows, 2 * kv_heads, scale=0.0)
+        for qb, got, kb, vb in zip(q, out, c.k, c.v):
+            n = len(kb)
+            want, size = ref.attention(qb, ref.cache_values(kb), ref.cache_values(vb), 0.0, [n - len(qb) + i + 1 for i in range(len(qb))])
+            assert (np.abs(got - want) <= (2.0 ** -11 + 2.0 ** -14) * size).all()
+    q, out = _attend_all(c, rows, 2 * kv_heads)
+    _check_cache(c, q, out)
+
+
+def test_more_steps_than_workgroups_twice():
+    c = Cached([650 + 3 * b for b in range(40)], 8, 64, 32, seed=3)
+    q, out = _attend_all(c, [1] * 40, 8)
+    _check_cache(c, q, out)
+
+
+def test_more_pages_than_a_wavefront_holds_at_once():
+    """The same 40 pages over and over, in random order, some absent: every workgroup has 65 steps and more of one sequence."""
+    n, count = 33000, 130
+    c = Cached([1280], 1, 64, 32, seed=15)
+    held = [np.concatenate([ref.cache_values(x[0]), np.zeros((32, 1, 64))]).reshape(41, 32, 64) for x in (c.k, c.v)]
+    place = {page: i for i, page in enumerate(c.pages[0])}
+    table = c.rng.integers(0, c.n_pages, (count, -(-n // 32))).astype(np.int32)
+    table[c.rng.random(table.shape) < 0.1] = -1
+    q = normal(c.rng, count, 2, 64)
+    out = gq.gqsa_cache_attend(c.cache, dev(q), dev(table), ints(*[n - 7 * b for b in range(count)])).cpu().numpy()
+    for b in range(0, count, 3):
+        at = np.array([place.get(page, 40) for page in table[b]])
+        there = np.repeat(at < 40, 32)[:n - 7 * b]
+        k, v = (x[at].reshape(-1, 1, 64)[:n - 7 * b][there] for x in held)
+        want, size = ref.attention(q[b:b + 1], k, v, 0.125, [len(k)])
+        _check_attended(out[b:b + 1], want, size, len(k), v)
+
+
 def test_one_row_per_sequence_and_strided_queries():
     c = Cached([100, 7], 2, 128, 32, seed=8)
     joint = normal(c.rng, 2, 8, 128)
@@ -439,6 +488,18 @@ def test_attention_over_prompts(dim, q_heads, kv_heads, q_rows, k_rows):
     assert torch.equal(gq.gqsa_prompt_attend(*args), out)
 
 
+@pytest.mark.parametrize("dim, q_heads, kv_heads, q_rows, k_rows", [
+    (64, 64, 4, [300, 130], [300, 500]),
+    (128, 96, 32, [200, 1, 70], [260, 300, 40]),
+    (128, 270, 2, [129], [200]),
+])
+def test_attention_over_prompts_with_many_heads(dim, q_heads, kv_heads, q_rows, k_rows):
+    rng = np.random.default_rng(q_heads)
+    q, k, v, qs, ks = _prompts(rng, q_rows, k_rows, q_heads, kv_heads, dim)
+    out = gq.gqsa_prompt_attend(dev(q), dev(k), dev(v), dev(qs), dev(ks)).cpu().numpy()
+    _check_prompts(out, q, k, v, qs, ks, dim ** -0.5)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 def test_prompt_scales(scale):
     q, k, v, qs, ks = _prompts(np.random.default_rng(1), [70, 9], [70, 20], 2, 1, 64)
@@ -477,6 +538,22 @@ def test_keys_and_values_that_a_row_does_not_see_have_no_effect(dim):
     assert np.array_equal(out[~touched], clean[~touched])
     assert not np.isfinite(out[touched]).any()
     assert (out[88:90, 2:, 3] == -np.inf).all() and (out[90 + 40:90 + 100, :2, 5] == np.inf).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_what_a_row_does_not_see_with_many_heads(dim):
+    rng = np.random.default_rng(dim + 1)
+    q, k, v, qs, ks = _prompts(rng, [90, 150], [90, 170], 96, 2, dim)
+    clean = gq.gqsa_prompt_attend(dev(q), dev(k), dev(v), dev(qs), dev(ks)).cpu().numpy()
+    k2, v2 = k.copy(), v.copy()
+    k2[90 + 160, 0] = np.nan                                 # seen from row 140 of the second sequence on
+    v2[90 + 60, 0, 5], v2[90 + 61, 1, 7], v2[90 + 130, 1, 7] = np.inf, -np.inf, np.inf      # from rows 40, 41 and 110 on
+    out = gq.gqsa_prompt_attend(dev(q), dev(k2), dev(v2), dev(qs), dev(ks)).cpu().numpy()
+    touched = np.zeros(q.shape, bool)
+    touched[90 + 140:, :48] = touched[90 + 40:, :48, 5] = touched[90 + 41:, 48:, 7] = True
+    assert np.array_equal(out[~touched], clean[~touched])
+    assert np.isnan(out[90 + 140:, :48]).all() and (out[90 + 40:90 + 140, :48, 5] == np.inf).all()
+    assert (out[90 + 41:90 + 110, 48:, 7] == -np.inf).all() and np.isnan(out[90 + 110:, 48:, 7]).all()
 
 
 def test_prompt_starts_beyond_their_arrays_stay_inside():
