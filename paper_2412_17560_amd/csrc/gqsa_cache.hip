@@ -657,6 +657,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
         const unsigned ahead = (head0 + (lane & 15)) / per;
         const int row = token0 + ahead, q_head = head * per + (head0 + (lane & 15) - ahead * per);
         const int limit = is_row ? before + row + 1 : 0;     // tokens it sees
+        // (an infinity as NaN: it makes a row NaN, which scores of -infinity only would not)
         half8_t q[D / 32];
         const uint16_t* q_at = a.q.data + int64_t{seq.start + row} * a.q.row + q_head * a.q.head + 8 * quad;
 #pragma unroll
@@ -664,6 +665,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
             q[g] = half8_t{};
             if (is_row) q[g] = *reinterpret_cast<const half8_t*>(q_at + 32 * g);
             if (a.negate) q[g] = -q[g];
+            q[g] += q[g] - q[g];
         }
         const int least = before + token0 + 1, most = before + token0 + (head0 + rows - 1) / per + 1;    // tokens that the block's first and last row see
         const int tiles = uniform(min((max(most, 0) + kTileTokens - 1) / kTileTokens, to * step_tiles));

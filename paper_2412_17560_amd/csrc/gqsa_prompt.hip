@@ -276,7 +276,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
             for (int r = 0; r < 16; ++r) out[d][r] = f * out[d][r] + g * meet[(2 + 16 * d + r) * 64];
     }
     if (row >= n_q) return;
-    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;       // (a row without keys: all sums are 0)
+    const float inverse = sees > 0 ? 1.0f / sum : 0.0f;       // (a row without keys: all sums are 0; one with scores of -infinity only is NaN)
     uint16_t* to = c.out.data + (int64_t{q_start} + row) * c.out.row + head * c.out.head + 4 * half;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)

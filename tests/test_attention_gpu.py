@@ -374,6 +374,15 @@ def test_nan_keys_reach_the_rows_that_see_them():
     assert np.isfinite(out[0]).all() and np.isnan(out[1:]).all()
 
 
+def test_infinite_queries_are_nan_where_they_see_a_token():
+    c = Cached([40, 0, 300], 1, 64, 32, seed=16)
+    q = normal(c.rng, 3, 3, 64)
+    q[:, 0, 5], q[:, 1, 9] = np.inf, -np.inf
+    out = gq.gqsa_cache_attend(c.cache, dev(q), dev(c.pages), ints(*c.lengths())).cpu().numpy()
+    assert np.isnan(out[::2, :2]).all() and (out[1] == 0).all()
+    _check_cache(c, [x[None, 2:] for x in q], [x[None, 2:] for x in out])
+
+
 def test_absent_pages_are_absent_tokens():
     c = Cached([300], 2, 64, 32, seed=5)
     c.pages[0, 2], c.pages[0, 5] = -1, c.n_pages
@@ -538,6 +547,22 @@ def test_keys_and_values_that_a_row_does_not_see_have_no_effect(dim):
     assert np.array_equal(out[~touched], clean[~touched])
     assert not np.isfinite(out[touched]).any()
     assert (out[88:90, 2:, 3] == -np.inf).all() and (out[90 + 40:90 + 100, :2, 5] == np.inf).all()
+
+
+def test_prompt_scores_of_infinity():
+    """All scores of a row -infinity, or one +infinity: NaN, as the formula's; some -infinity: weights of 0."""
+    q, k, v, qs, ks = _prompts(np.random.default_rng(5), [3, 200], [2, 200], 2, 1, 64)
+    q, k = np.abs(q) + np.float16(0.1), np.abs(k) + np.float16(0.1)
+    k[0, 0, 7] = k[2, 0, 3] = k[100, 0, 1] = -np.inf
+    out = gq.gqsa_prompt_attend(dev(q), dev(k), dev(v), dev(qs), dev(ks)).cpu().numpy()
+    assert (out[0] == 0).all() and np.isnan(out[1]).all() and np.isnan(out[3]).all()
+    for r, at in [(2, [1]), *[(3 + r, [2 + i for i in range(r + 1) if i not in (0, 98)]) for r in (1, 60, 98, 99, 199)]]:
+        want, size = ref.attention(q[r:r + 1], k[at], v[at], 0.125, [len(k[at])])
+        _check_attended(out[r:r + 1], want, size, len(k[at]), v[at])
+    k[np.isinf(k)] = 1
+    q[50, 0, 3] = np.inf
+    out = gq.gqsa_prompt_attend(dev(q), dev(k), dev(v), dev(qs), dev(ks)).cpu().numpy()
+    assert np.isnan(out[50, 0]).all() and np.isfinite(np.delete(out.reshape(-1, 64), 100, axis=0)).all()
 
 
 @pytest.mark.parametrize("dim", [64, 128])
