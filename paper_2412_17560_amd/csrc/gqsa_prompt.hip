@@ -275,9 +275,13 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
 #pragma unroll
             for (int r = 0; r < 16; ++r) out[d][r] = f * out[d][r] + g * meet[(2 + 16 * d + r) * 64];
     }
-    if (row >= n_q) return;
-    const float inverse = sees > 0 ? 1.0f / sum : 0.0f;       // (a row without keys: all sums are 0; one with scores of -infinity only is NaN)
-    uint16_t* to = c.out.data + (int64_t{q_start} + row) * c.out.row + head * c.out.head + 4 * half;
+    // (from the lane's number anew: kept from the loop's start, it would take registers from the loop, 2 %)
+    int own_lane = lane;
+    asm volatile("" : "+v"(own_lane));
+    const int own_row = wave_row0 + (own_lane & 31);
+    if (own_row >= n_q) return;
+    const float inverse = own_row + behind >= 0 ? 1.0f / sum : 0.0f;       // (a row without keys: all sums are 0; one with scores of -infinity only is NaN)
+    uint16_t* to = c.out.data + (int64_t{q_start} + own_row) * c.out.row + head * c.out.head + 4 * (own_lane >> 5);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
