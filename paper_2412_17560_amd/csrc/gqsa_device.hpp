@@ -35,6 +35,19 @@ __device__ __forceinline__ unsigned running_sum(unsigned v)
     return add_from<0x143, 0xC>(v);     // lane 31, into the third and the fourth
 }
 
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ unsigned most_from(unsigned v)
+{
+    return max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CONTROL, ROWS, 0xF, false)));
+}
+
+// The largest of all lanes' numbers.
+__device__ __forceinline__ unsigned largest(unsigned v)
+{
+    v = most_from<0x118, 0xF>(most_from<0x114, 0xF>(most_from<0x112, 0xF>(most_from<0x111, 0xF>(v))));
+    return __builtin_amdgcn_readlane(static_cast<int>(most_from<0x143, 0xC>(most_from<0x142, 0xA>(v))), 63);
+}
+
 // Units dealt to the sequences in order, count(seq) to a sequence that load(b) has fetched (a struct of three ints): how many there are (0 if it is 2^31 or
 // more, which no sound call has), and to which sequence a unit belongs and as the how manieth.  Lane l holds the l-th sequence, so that
 // no load waits for another.  Called by whole wavefronts; sequences beyond the first 64 are fetched again by locate().

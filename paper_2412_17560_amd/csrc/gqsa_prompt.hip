@@ -72,9 +72,33 @@ __device__ __forceinline__ bool some_not_finite(const uint16_t* tile)
     return (over & 0x80008000u) != 0;
 }
 
+// The slot-th of the blocks of up to 64 sequences in the order of the keys they see, the most first: `level` is how many times ROWS those are, the last block of
+// lane l's sequence is at level ends of lane l, the one before it a level lower, and so on.
+template <int ROWS, typename Deal>
+__device__ __forceinline__ auto longest_first(const Deal& deal, unsigned slot, int* b, int* block)
+{
+    const unsigned ends = max(static_cast<unsigned>(deal.seq.length + ROWS - 1) / ROWS, deal.own);
+    const auto above = [&](unsigned level) { return Deal::last(running_sum(min(ends > level ? ends - level : 0u, deal.own))); };
+    unsigned low = 0, level = largest(deal.own ? ends : 0u), before = 0;       // above(low) > slot, above(level) = before <= slot
+    while (level - low > 1) {
+        const unsigned middle = (low + level) / 2, n = above(middle);
+        if (n > slot) low = middle;
+        else level = middle, before = n;
+    }
+    const uint64_t there = __builtin_amdgcn_ballot_w64(ends >= level && level + deal.own > ends);
+    const unsigned rank = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(there >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(there), 0));
+    const int who = __builtin_ctzll(there & __builtin_amdgcn_ballot_w64(rank == slot - before));
+    *b = who;
+    *block = __builtin_amdgcn_readlane(static_cast<int>(deal.own + level - ends), who) - 1;
+    auto seq = deal.seq;
+    seq.start = __builtin_amdgcn_readlane(seq.start, who), seq.rows = __builtin_amdgcn_readlane(seq.rows, who);
+    seq.length = __builtin_amdgcn_readlane(seq.length, who);
+    return seq;
+}
+
 // SPLIT: how many wavefronts share their rows, each with every SPLIT-th part of a tile's keys.  With 2 a workgroup has 64 rows instead of 128.
 template <int D, int SPLIT>
-__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool negate)
+__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool negate, bool mixed)
 {
     constexpr int kGroups = kWaves / SPLIT, kBlockRows = kGroups * kWaveRows;
     constexpr int kPieces = 2 / SPLIT;               // runs of 32 keys of a tile that a wavefront takes
@@ -90,8 +114,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
     };
     const auto start_of = [](const int32_t* starts, int64_t n, int b) { return min(max(starts[b], 0), static_cast<int>(n)); };
     const auto rows_of = [&](const int32_t* starts, int64_t n, int b) { return max(min(starts[b + 1], static_cast<int>(n)) - start_of(starts, n, b), 0); };
-    // Heads vary fastest, those of a group on one XCD (workgroup i runs on XCD i % 8), the last blocks of a sequence -- those with the
-    // most keys -- come first.
+    // Heads vary fastest, those of a group on one XCD (workgroup i runs on XCD i % 8); blocks with more keys come first, of each
+    // sequence or (mixed) of all, so that what runs last is short.
     const unsigned slot = blockIdx.x / static_cast<unsigned>(c.q_heads), of = blockIdx.x % static_cast<unsigned>(c.q_heads);
     const int head = c.q_heads % 8 == 0 ? of % 8 * (c.q_heads / 8) + of / 8 : of;
     const auto deal = deal_out<Prompt>(c.n_seqs, lane, [&](int b) {
@@ -99,7 +123,9 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
     }, [](const Prompt& p) { return static_cast<unsigned>(p.rows + kBlockRows - 1) / kBlockRows; });
     if (slot >= deal.total) return;
     int b, block;
-    const Prompt prompt = deal.locate(deal.total - 1 - slot, &b, &block);
+    Prompt prompt;
+    if (mixed) prompt = longest_first<kBlockRows>(deal, slot, &b, &block);
+    else prompt = deal.locate(deal.total - 1 - slot, &b, &block);
     const int q_start = prompt.start, n_q = prompt.rows, n_k = prompt.length, k_start = start_of(c.k_starts, c.n_k_rows, b);
     const int behind = n_k - n_q;                    // row r sees keys 0 .. r + behind
     const int row0 = block * kBlockRows, wave_row0 = row0 + group * kWaveRows;
@@ -313,14 +339,21 @@ gqsa_status_t prompt_attend(const PromptCall& call, void* stream)
     const bool split = c.n_k_rows > kTileKeys * int64_t{c.n_seqs} && whole <= (c.n_k_rows >= int64_t{1000} * c.n_seqs ? 512 : 256);
     const int64_t blocks = split ? half : whole;
     if (blocks > (int64_t{1} << 23)) return GQSA_ERR_SHAPE;
+    // Blocks of all sequences in the order of their keys, not one sequence after the other, where more of them than run at once would otherwise end with a
+    // long one -- us of either order, ragged lengths up to: 6 x 900, 32 heads 50 / 44.7; 12 x 800 53.1 / 48.7; 30 x 500 53.6 / 50.5; 3 x 1500 62.8 / 60; 20 x 1000, 14 heads of 64
+    // 47.7 / 39 -- but not where the keys and values that an XCD's workgroups are at would then pass its L2 (4 MiB): 7 x 2500, 40 heads 295 / 301; 12 x 3000 554 / 571;
+    // and not where a sequence is a block or so: 64 x 40 21.8 / 22.4.
+    const int64_t heads_at_once = (c.kv_heads + 7) / 8;
+    const bool mixed = !split && c.n_seqs > 1 && c.n_seqs <= 64 && blocks > 512 && c.n_k_rows >= int64_t{kWaves} * kWaveRows * c.n_seqs &&
+                       c.n_k_rows * c.head_dim * 4 * heads_at_once <= (int64_t{4} << 20);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid(static_cast<unsigned>(blocks));
     if (c.head_dim == 128) {
-        if (split) hipLaunchKernelGGL((prompt_kernel<128, 2>), grid, dim3(kThreads), 0, s, c, negate);
-        else hipLaunchKernelGGL((prompt_kernel<128, 1>), grid, dim3(kThreads), 0, s, c, negate);
+        if (split) hipLaunchKernelGGL((prompt_kernel<128, 2>), grid, dim3(kThreads), 0, s, c, negate, mixed);
+        else hipLaunchKernelGGL((prompt_kernel<128, 1>), grid, dim3(kThreads), 0, s, c, negate, mixed);
     } else {
-        if (split) hipLaunchKernelGGL((prompt_kernel<64, 2>), grid, dim3(kThreads), 0, s, c, negate);
-        else hipLaunchKernelGGL((prompt_kernel<64, 1>), grid, dim3(kThreads), 0, s, c, negate);
+        if (split) hipLaunchKernelGGL((prompt_kernel<64, 2>), grid, dim3(kThreads), 0, s, c, negate, mixed);
+        else hipLaunchKernelGGL((prompt_kernel<64, 1>), grid, dim3(kThreads), 0, s, c, negate, mixed);
     }
     GQSA_HIP(hipGetLastError());
     return GQSA_OK;

@@ -501,6 +501,9 @@ def test_attention_over_prompts(dim, q_heads, kv_heads, q_rows, k_rows):
     (64, 64, 4, [300, 130], [300, 500]),
     (128, 96, 32, [200, 1, 70], [260, 300, 40]),
     (128, 270, 2, [129], [200]),
+    (64, 64, 2, [300, 5, 0, 130, 700], [300, 400, 0, 20, 701]),       # blocks of the sequences mixed
+    (128, 80, 8, [10, 400, 129, 128, 60, 257], [600, 400, 140, 128, 50, 257]),
+    (64, 33, 3, [150 + (37 * b) % 200 for b in range(40)], [180 + (37 * b) % 200 for b in range(40)]),
 ])
 def test_attention_over_prompts_with_many_heads(dim, q_heads, kv_heads, q_rows, k_rows):
     rng = np.random.default_rng(q_heads)
