@@ -109,7 +109,9 @@ gqsa_status_t gqsa_cache_read(gqsa_cache_t c, void* k_out, int64_t k_row_stride,
  *   q, out   [device] fp16 [n_rows, q_heads, head_dim]; q_heads a multiple of kv_heads, at most 1024; every row of out is written
  *            that belongs to a sequence
  *   scale    finite (GQSA_ERR_RANGE), head_dim^-0.5 usually
- * Every sequence may have any number of rows; the cache is read once per 16 rows of the heads of a group.  Results are bit-identical
+ * Every sequence may have any number of rows; the cache is read once per 16 rows of the heads of a group.  GQSA_ERR_SHAPE where n_rows times
+ * q_heads / kv_heads passes 2^30, or where the pages that the table has room for could be 2^31 steps of 128 tokens and more, over all rows and
+ * heads.  A query with an infinity or a NaN makes its row NaN.  Results are bit-identical
  * from run to run.  Can be captured (nothing is allocated, nothing is read back).
  */
 gqsa_status_t gqsa_cache_attend(gqsa_cache_t c, const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads,
@@ -123,7 +125,7 @@ gqsa_status_t gqsa_cache_attend(gqsa_cache_t c, const void* q, int64_t q_row_str
  * (more keys than queries: an earlier part of the prompt that has been seen already).  A row that sees no key is zero.
  *   q, out   [device] fp16 [n_q_rows, q_heads, head_dim];  k, v [device] fp16 [n_k_rows, kv_heads, head_dim]
  *   head_dim 64 or 128; q_heads a multiple of kv_heads (grouped heads as in gqsa_cache_attend), at most 1024; rows of k and of v
- *            at most 2^23 elements apart (GQSA_ERR_UNSUPPORTED)
+ *            at most 2^23 elements apart (GQSA_ERR_UNSUPPORTED); (n_q_rows / 128 + n_seqs) q_heads at most 2^23 (GQSA_ERR_SHAPE)
  * Keys and values that a row does not see have no effect on it, whatever they hold.
  */
 gqsa_status_t gqsa_prompt_attend(const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads, int64_t n_q_rows,

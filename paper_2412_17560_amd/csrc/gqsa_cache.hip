@@ -137,6 +137,8 @@ __device__ __forceinline__ Quantised<N> quantise(const half8_t (&x)[N / 8])
 // One workgroup per tile that gets rows, and head: 8 threads to a token.  The tile is put together in LDS -- a word of key codes is of one token, but one of
 // value codes of 8 -- and written in runs of 16 bytes; of a tile that keeps earlier tokens, only the new ones' words and halves are
 // written, and words of value codes that they share are read first (nobody else writes the tile).
+// Few tokens are a chain of waits (lengths and starts, the page's number, the rows, LDS): 1 token of 16 sequences and 32 heads takes 4.8 us, where an empty launch
+// takes 1.6.  Many are bound by that chain and by the arithmetic of 32 codes a thread: 8192 tokens of 8 heads of 128 take 16 us, 44 MB at 2.8 TB/s.
 template <int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(CopyArgs a)
 {
@@ -231,6 +233,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CopyArgs a)
     }
 }
 
+// The same deal.  A tile comes into LDS in runs of 16 bytes, as the codes of a token are spread over words of other tokens; bound by the same chain: 8192 tokens of
+// 8 heads of 128 take 13 us (3.4 TB/s), 1 of 16 sequences and 32 heads 3.4.
 template <int D>
 __global__ __launch_bounds__(kThreads) void read_kernel(CopyArgs a)
 {
@@ -516,6 +520,7 @@ struct Partials {
 constexpr int kHeld = 2;             // tiles that a wavefront holds: the one at work, and those under way
 constexpr int kAttendWaves = 4;      // wavefronts of a workgroup; a step: one tile for each
 
+// (32 / 16 / 8, us: 131072 tokens, 8 heads for 64 45.3 / 42.7 / 42.0; 32768 tokens, 1 for 16 17.8 / 14.5 / 14.5; 4 x 20000 tokens, 4 rows, 8 for 64 40.8 / 41.3 / 44.5)
 constexpr int kFan = 16;        // parts that one workgroup joins alone, unless they are themselves joined ones
 constexpr int kMostParts = (kAttendWorkgroups + kFan - 1) / kFan;       // of which there are up to so many
 static_assert(kMostParts >= kFan, "");
@@ -600,11 +605,21 @@ __device__ __forceinline__ int steps_of(const Sequence& q, int step_tiles)
     return max(static_cast<int>(static_cast<unsigned>(q.length + step_tiles * kTileTokens - 1) / static_cast<unsigned>(step_tiles * kTileTokens)), 1);
 }
 
+// Of 0 / 1 / 2 / 4 / 8 steps a workgroup, us: 143 tokens of 32 heads 7.4 / 6.45 / 6.45 / 6.4 / 6.4; 8 x 3000 tokens, 4 rows, 2 for 14 of 64 11.7 / 11.8 / 9.9 / 10.0 / 10.0;
+// 32768 tokens, 1 for 16 16.0 / 14.3 / 14.5 / 14.4 / 14.4; 131072, 8 for 64 44.2 / 43.6 / 42.7 / 43.8 / 43.8; 64 sequences of up to 40 tokens, 8 for 32 6.9 / 7.1 / 7.1 / 7.2 / 7.2.
 constexpr unsigned kFewSteps = 2;
 
 // The work is dealt by steps of 128 or 256 tokens, not by sequences or heads: of all steps, in the order sequence, head, block of 16 rows, token, every
 // workgroup takes a run, all of one length or one more.  Where a segment (one block of rows of one head) lies in several workgroups, each
 // leaves its maximum, sum and weighted sum in the workspace, and the last to arrive joins them in the order of the tokens.
+//
+// One row for a head of the cache is bound by memory: 16 x 4096 tokens of 32 heads of 128, 336 MB, take 65.5 us, 5.1 TB/s; the same with all tiles in the L2 caches
+// 49 us, which is what the vector instructions take (88 of them turn a tile's 1024 words of keys into numbers, 88 the values; a softmax of 16 x 32 scores 60; 16
+// products).  Several rows for a head hide nothing more: up to 16 cost what one costs, and every further 16 the instructions anew: 8 ragged sequences of up to 16003
+// tokens, 5 rows of 32 heads for 8, 84 MB, take 35.5 us, of which the words' decoding, done twice, is half.  (Two blocks of rows under one decoding took 46 us, for
+// want of registers -- 46 of them went to memory -- and with heads of 64, where there are enough, 16.9 instead of 12.5: too few wavefronts with too long a chain.)
+// A single short sequence is a chain of waits: 143 tokens of 32 heads 6.4 us.  512 workgroups are what fits at once: with 1024, half of them ran after the others
+// (121 us instead of 75); with 3 or 4 wavefronts a SIMD, the state goes to memory.
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
 {

@@ -5,6 +5,12 @@
 // memory straight into LDS, one tile ahead of the one at work.  Both products are 32x32x16 ones, taken the other way round --
 // S^T = K Q^T, O^T = V^T P^T -- because then a lane holds scores of one query row only (its maximum and sum need one exchange, between the two
 // halves of the wavefront) and holds them as the second product wants its operand; V^T comes out of LDS by transposing reads.
+//
+// Long prompts are bound by what the matrix cores and the vector units do in turn: 8192 tokens of 32 heads of 128 for 8 (550 GFLOP) take 558 to 595 us, by the card's
+// clock, 985 to 925 TFLOP/s, where a large library product of fp16 reaches 1113.  Without its copies into LDS the kernel takes 502 us, copies alone 217.  Each
+// exponential costs as much as two other instructions, and a tile has 64 of them for every 64 lanes' row; with the weights' sum by dot products of what the second
+// product takes, and the reference that follows only now and then, little else is left beside it.  Ragged batches pay for the diagonal's tiles: 7 sequences of up to 2500
+// tokens, 40 heads for 8, 288 to 308 us, 735 to 785 TFLOP/s of the scores that the mask leaves.  One short prompt is a chain of waits: 15 tokens of 32 heads 5.3 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -329,10 +335,10 @@ gqsa_status_t prompt_attend(const PromptCall& call, void* stream)
     c.scale = std::max(std::fabs(c.scale) * 1.44269504088896341f, 1e-30f);
     // Few workgroups: rows shared by two wavefronts, so that there are twice as many.  us of own / shared rows, heads of 128, by the workgroups of 128 rows
     // (bound below):
-    //   keys of 1000 and more: 128 rows 1 x 128 + 2000 keys x 32 heads 46.9 / 35.0; 160: 512 + 2000 keys 59.7 / 44.2; 224: 2000 x 14 heads 52.5 / 39.3; 352: 1300 x 32
-    //     38.4 / 34.2; 384: 1500 x 32 43.4 / 39.5; 448: 4000 x 14 100 / 89.5; 576: 1024 x 64 35.7 / 40.0;
-    //   fewer: 96: 256 x 32 12.5 / 11.5; 192: 700 x 32 21.6 / 19.4; 320: 4 x 194 x 32 14.9 / 14.1, 8 x 100 x 32 (352) 10.5 / 11.8; 384: 700 x 64 25.5 / 28.2;
-    //     392: 2 x 800 x 28 28.7 / 30.0; one tile of keys (15 x 32) 7.8 / 8.4, 16 x 64 x 14 8.1 / 9.2.
+    //   keys of 1000 and more: 32: 1 row, 2000 keys, 32 heads 43.7 / 32.5; 224: 2000 x 14 heads 49.9 / 38.1; 256: 2000 rows, 4000 keys, 16 heads 96 / 81; 320: 1000 x 40
+    //     30.4 / 25.5; 352: 1300 x 32 36.3 / 30.9; 384: 1500 x 32 41.5 / 35.3; 448: 4000 x 14 97.6 / 84.2; 576: 1024 x 64 34.2 / 35.7; 2080: 8192 x 32 565 / 671;
+    //   fewer: 64: 128 x 32 8.2 / 7.7; 96: 256 x 32 11.0 / 9.7; 192: 700 x 32 19.8 / 18.1; 256: 900 x 32 25.0 / 22.4; 320: 4 x 194 x 32 12.5 / 12.2; 384: 700 x 64 24.0 / 23.6;
+    //     392: 2 x 800 x 28 27.5 / 27.3; 448: 8 x 100 x 32 8.6 / 9.5; one tile of keys (15 x 32) 5.4 / 5.8, 16 x 64 x 14 6.6 / 7.5.
     // (Four tiles in LDS instead of two, where every workgroup has a compute unit for itself, took 1.1 to 1.25 times as long.)
     const auto blocks_of = [&](int rows) { return (c.n_q_rows / rows + c.n_seqs) * c.q_heads; };      // no fewer than there are
     const int64_t whole = blocks_of(kWaves * kWaveRows), half = blocks_of(kWaves * kWaveRows / 2);

@@ -4,6 +4,7 @@
 // few.  A lane holds two runs of 8 elements of a head whose elements are each other's partners in the rotation (runs p and
 // p + rotary_dim / 16, or two neighbouring runs), so that the rotation needs no exchange between lanes and the norm's sum
 // one over the head_dim / 16 lanes of a head; (c, s) of its 8 pairs stay in registers over all heads of a row.
+// 8192 rows of 72 heads of 128 take 62 us, 4.9 TB/s of the 5.2 that a large copy reaches; one row 3.0 us, where an empty launch takes 1.6.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -121,7 +122,7 @@ void launch(const RotateCall& c, hipStream_t s)
     constexpr int kHeadsAtOnce = 64 / LANES;
     const int sets = (c.q_heads + c.k_heads + kHeadsAtOnce - 1) / kHeadsAtOnce;
     // A wavefront keeps its row's part of the table in registers over all the heads it takes, so few to a row read it less often; but there should be some
-    // four times as many as the chip holds at once (7 a SIMD), or the last of them run alone: 8192 rows of 72 heads of 128 take 73.6 us with
+    // four times as many as the chip holds at once (7 a SIMD), or the last of them run alone: 8192 rows of 72 heads of 128 took 73.6 us with
     // 8192 wavefronts, 66.0, 63.1 and 62.6 with 16384, 32768 and all of one set of heads each; 16384 rows of 40 heads of 64 41.9, 41.6, 39.5, 41.0.
     const int waves_per_row = static_cast<int>(std::min<int64_t>(sets, std::max<int64_t>(1, 32768 / c.n_rows)));
     const int64_t waves = c.n_rows * waves_per_row;
