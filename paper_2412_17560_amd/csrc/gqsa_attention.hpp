@@ -7,12 +7,13 @@
 
 #include "gqsa_attention.h"
 
-// (used where the HIP runtime is included)
+// (used where the HIP runtime is included; an error that has been reported is taken off the runtime's record, where the next launch would find it)
 #define GQSA_HIP(call)                                                                   \
     do {                                                                                 \
         const hipError_t e_ = (call);                                                    \
         if (e_ != hipSuccess) {                                                          \
             std::fprintf(stderr, "libgqsa: %s: %s\n", #call, hipGetErrorString(e_));    \
+            (void)hipGetLastError();                                                     \
             return GQSA_ERR_HIP;                                                         \
         }                                                                                \
     } while (0)

@@ -215,6 +215,13 @@ def test_cache_info():
     gq.gqsa_cache_free(c)
 
 
+def test_a_cache_that_does_not_fit_leaves_no_error_behind():
+    with pytest.raises(RuntimeError):
+        gq.gqsa_cache_create(2 ** 30, 4096, 1024, 128)
+    assert int(torch.ones(5, device="cuda").sum()) == 5
+    Cached([40], 1, 64, 32).check()
+
+
 # ----------------------------------------------------------------------------- attention over the cache
 def _check_attended(got, want, size, tokens, values):
     """Each weight and the result are rounded to fp16 (2^-11 each, of what they make up), a weight below the normal range by up to 2^-25 of the
