@@ -616,8 +616,9 @@ constexpr unsigned kFewSteps = 2;
 // One row for a head of the cache is bound by memory: 16 x 4096 tokens of 32 heads of 128, 336 MB, take 65.5 us, 5.1 TB/s; the same with all tiles in the L2 caches
 // 49 us, which is what the vector instructions take (88 of them turn a tile's 1024 words of keys into numbers, 88 the values; a softmax of 16 x 32 scores 60; 16
 // products).  Several rows for a head hide nothing more: up to 16 cost what one costs, and every further 16 the instructions anew: 8 ragged sequences of up to 16003
-// tokens, 5 rows of 32 heads for 8, 84 MB, take 35.5 us, of which the words' decoding, done twice, is half.  (Two blocks of rows under one decoding took 46 us, for
-// want of registers -- 46 of them went to memory -- and with heads of 64, where there are enough, 16.9 instead of 12.5: too few wavefronts with too long a chain.)
+// tokens, 5 rows of 32 heads for 8, 84 MB, take 35.5 us, of which the words' decoding, done twice, is half.  (Two blocks of rows under one decoding,
+// with queries in LDS: 38 us here, 29.5 instead of 35.9 for 32 sequences of 2000 tokens and 3 rows, but 23.7 instead of 14.8 for 1 head for 32 over 32768 tokens, where the
+// joins' work doubles.  Workgroups of both blocks beside each other on one XCD: 36.7.)
 // A single short sequence is a chain of waits: 143 tokens of 32 heads 6.4 us.  512 workgroups are what fits at once: with 1024, half of them ran after the others
 // (121 us instead of 75); with 3 or 4 wavefronts a SIMD, the state goes to memory.
 template <int D, int WAVES>
