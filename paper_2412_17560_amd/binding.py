@@ -484,8 +484,8 @@ def _heads(t, what: str):
     try:
         rows, heads, dim = t.shape
         row, head, one = t.stride()
-        if one == 1 and t.dtype is _HALF and t.is_cuda:
-            # (torch lets the distance of a dimension of size 1 be anything)
+        if (one == 1 or rows == 0) and t.dtype is _HALF and t.is_cuda:
+            # (torch lets the distance of a dimension of size 1 be anything, and all of them without rows)
             return t.data_ptr(), row if rows > 1 else 0, head if heads > 1 else 0, rows, heads, dim
     except (AttributeError, TypeError, ValueError):
         pass

@@ -601,6 +601,13 @@ def test_prompt_starts_beyond_their_arrays_stay_inside():
     _check_prompts(out[10:50], q, k, v, [0, 30, 40], [0, 30, 40], 0.125)
 
 
+def test_prompts_without_any_key():
+    q = dev(normal(np.random.default_rng(2), 5, 4, 64))
+    for k in (torch.zeros((0, 2, 64), dtype=torch.float16, device="cuda"), torch.zeros(0, dtype=torch.float16, device="cuda").as_strided((0, 2, 64), (0, 0, 0))):
+        out = gq.gqsa_prompt_attend(q, k, k, ints(0, 3, 5), ints(0, 0, 0), out=torch.ones_like(q))
+        assert (out == 0).all()
+
+
 def test_prompt_through_the_cache_is_the_prompt():
     """A prompt's second part attends to the first as the cache gives it back: the same as the plain attention over those values."""
     c = Cached([200], 2, 128, 64, seed=21)
