@@ -44,6 +44,19 @@ constexpr int tile_bytes(int head_dim) { return kTileTokens * head_dim + 2 * kTi
 constexpr int kAttendWorkgroups = 512;      // the most workgroups of one attention over the cache: two to a compute unit
 constexpr int kRowBlock = 16;               // query rows (rows of a sequence times the heads of a group) per product
 
+// The rows that a sequence has, from the two ends that an array on the device gives, which may be anything: none outside 0 .. n - 1 (n at most 2^25).  Both
+// ends are brought into 0 .. n before one is taken off the other, as their difference may not fit 32 bits.
+struct Rows {
+    int start, count;
+};
+constexpr Rows rows_between(int first, int end, int64_t n)
+{
+    const int most = static_cast<int>(n);
+    const int start = first < 0 ? 0 : first < most ? first : most;
+    const int stop = end < start ? start : end < most ? end : most;
+    return {start, stop - start};
+}
+
 // Where the rows, pages and lengths of a call's sequences are.
 struct Sequences {
     const int32_t *pages, *lengths, *row_starts;

@@ -46,11 +46,10 @@ struct Sequence {
 
 __device__ __forceinline__ Sequence sequence(const Sequences& s, int page_shift, int b)
 {
-    const int n = static_cast<int>(s.n_rows);
-    const int first = s.row_starts ? s.row_starts[b] : b, end = s.row_starts ? s.row_starts[b + 1] : b + 1;
+    const Rows rows = rows_between(s.row_starts ? s.row_starts[b] : b, s.row_starts ? s.row_starts[b + 1] : b + 1, s.n_rows);
     Sequence q;
-    q.start = min(max(first, 0), n);
-    q.rows = max(min(end, n) - q.start, 0);
+    q.start = rows.start;
+    q.rows = rows.count;
     const int64_t most = int64_t{s.max_pages} << page_shift;
     q.length = static_cast<int>(min(static_cast<int64_t>(max(s.lengths[b], 0)), min(most, int64_t{INT_MAX - 4096})));
     return q;

@@ -118,21 +118,21 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
     struct Prompt {
         int start, rows, length;       // query rows, and where they start; keys
     };
-    const auto start_of = [](const int32_t* starts, int64_t n, int b) { return min(max(starts[b], 0), static_cast<int>(n)); };
-    const auto rows_of = [&](const int32_t* starts, int64_t n, int b) { return max(min(starts[b + 1], static_cast<int>(n)) - start_of(starts, n, b), 0); };
+    const auto rows_of = [](const int32_t* starts, int64_t n, int b) { return rows_between(starts[b], starts[b + 1], n); };
     // Heads vary fastest, those of a group on one XCD (workgroup i runs on XCD i % 8); blocks with more keys come first, of each
     // sequence or (mixed) of all, so that what runs last is short.
     const unsigned slot = blockIdx.x / static_cast<unsigned>(c.q_heads), of = blockIdx.x % static_cast<unsigned>(c.q_heads);
     const int head = c.q_heads % 8 == 0 ? of % 8 * (c.q_heads / 8) + of / 8 : of;
     const auto deal = deal_out<Prompt>(c.n_seqs, lane, [&](int b) {
-        return Prompt{start_of(c.q_starts, c.n_q_rows, b), rows_of(c.q_starts, c.n_q_rows, b), rows_of(c.k_starts, c.n_k_rows, b)};
+        const Rows q_rows = rows_of(c.q_starts, c.n_q_rows, b);
+        return Prompt{q_rows.start, q_rows.count, rows_of(c.k_starts, c.n_k_rows, b).count};
     }, [](const Prompt& p) { return static_cast<unsigned>(p.rows + kBlockRows - 1) / kBlockRows; });
     if (slot >= deal.total) return;
     int b, block;
     Prompt prompt;
     if (mixed) prompt = longest_first<kBlockRows>(deal, slot, &b, &block);
     else prompt = deal.locate(deal.total - 1 - slot, &b, &block);
-    const int q_start = prompt.start, n_q = prompt.rows, n_k = prompt.length, k_start = start_of(c.k_starts, c.n_k_rows, b);
+    const int q_start = prompt.start, n_q = prompt.rows, n_k = prompt.length, k_start = rows_of(c.k_starts, c.n_k_rows, b).start;
     const int behind = n_k - n_q;                    // row r sees keys 0 .. r + behind
     const int row0 = block * kBlockRows, wave_row0 = row0 + group * kWaveRows;
     const int row = wave_row0 + (lane & 31);

@@ -1,0 +1,72 @@
+"""Where the operators between the q/k/v and the o product could go wrong at the edge of what they take: against float64, on the GPU."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import paper_2412_17560_amd as gq
+from oracle import attention as ref
+from test_attention_gpu import Cached, _check_attended, dev, ints, normal
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+LEAST, MOST = -2 ** 31, 2 ** 31 - 1
+
+
+# ----------------------------------------------------------------------------- arrays on the device that hold anything
+def _between(starts, n):
+    """The rows of each sequence that are there."""
+    return [range(max(a, 0), max(min(b, n), max(a, 0))) for a, b in zip(starts, starts[1:])]
+
+
+STARTS = [[2, LEAST, 3], [5, LEAST, MOST], [MOST, LEAST, 2], [LEAST, 1, LEAST], [1, -1, LEAST + 1], [MOST, MOST - 1, LEAST]]
+
+
+@pytest.mark.parametrize("starts", STARTS)
+def test_starts_whose_difference_passes_32_bits_cache(starts):
+    c = Cached([64, 40], 1, 64, 32, seed=11)
+    n = 6
+    q = normal(c.rng, n, 2, 64)
+    room = torch.full((n + 20, 2, 64), 4.0, dtype=torch.float16, device="cuda")
+    gq.gqsa_cache_attend(c.cache, dev(q), dev(c.pages), ints(*c.lengths()), ints(*starts), out=room[10:10 + n])
+    kv = torch.full((n + 20, 1, 64), 4.0, dtype=torch.float16, device="cuda")
+    kv2 = kv.clone()
+    gq.gqsa_cache_read(c.cache, dev(c.pages), ints(*c.lengths()), ints(*starts), kv[10:10 + n], kv2[10:10 + n])
+    out, kv, kv2 = (t.cpu().numpy() for t in (room, kv, kv2))
+    left = np.ones(n + 20, bool)
+    for b, rows in enumerate(_between(starts, n)):
+        for i, r in enumerate(rows):
+            left[10 + r] = False
+            token = len(c.k[b]) - len(rows) + i
+            hk, hv = ref.cache_values(c.k[b]), ref.cache_values(c.v[b])
+            want, size = ref.attention(q[r:r + 1], hk, hv, 0.125, [token + 1])
+            _check_attended(out[10 + r:11 + r], want, size, len(hk), hv)
+            assert np.array_equal(kv[10 + r], hk[token]) and np.array_equal(kv2[10 + r], hv[token])
+    assert (out[left] == 4).all() and (kv[left] == 4).all() and (kv2[left] == 4).all()
+    x = normal(c.rng, n, 1, 64)
+    gq.gqsa_cache_append(c.cache, dev(x), dev(x), dev(c.pages), ints(*c.lengths()), ints(*starts))
+    for b, rows in enumerate(_between(starts, n)):          # the last tokens are these rows now, everything else is what it was
+        if len(rows):
+            c.k[b][-len(rows):] = c.v[b][-len(rows):] = x[rows.start:rows.stop]
+    c.check()
+
+
+@pytest.mark.parametrize("heads", [2, 96])          # rows shared by two wavefronts or not
+@pytest.mark.parametrize("q_starts, k_starts", [*[(s, [0, 40, 70]) for s in STARTS], *[([0, 4, 6], [10 * v if abs(v) < 9 else v for v in s]) for s in STARTS]])
+def test_starts_whose_difference_passes_32_bits_prompts(heads, q_starts, k_starts):
+    rng = np.random.default_rng(3)
+    n, keys = 6, 70
+    q, k, v = normal(rng, n, heads, 64), normal(rng, keys, 1, 64), normal(rng, keys, 1, 64)
+    room = torch.full((n + 20, heads, 64), 4.0, dtype=torch.float16, device="cuda")
+    gq.gqsa_prompt_attend(dev(q), dev(k), dev(v), ints(*q_starts), ints(*k_starts), out=room[10:10 + n])
+    out = room.cpu().numpy()
+    left = np.ones(n + 20, bool)
+    for rows, seen in zip(_between(q_starts, n), _between(k_starts, keys)):
+        if not len(rows):
+            continue
+        left[10 + rows.start:10 + rows.stop] = False
+        at, kb, vb = slice(rows.start, rows.stop), k[seen.start:seen.stop], v[seen.start:seen.stop]
+        want, size = ref.attention(q[at], kb, vb, 0.125, [len(seen) - len(rows) + i + 1 for i in range(len(rows))])
+        _check_attended(out[10 + rows.start:10 + rows.stop], want, size, len(seen), vb)
+    assert (out[left] == 4).all()
