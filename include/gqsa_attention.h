@@ -14,8 +14,8 @@
  *
  * Several sequences lie one behind the other in the rows: sequence b has the rows row_starts[b] .. row_starts[b + 1] - 1
  * (row_starts [device] int32[n_seqs + 1], or NULL: one row per sequence).  Values on the device cannot be refused by the host,
- * so the kernels bound them: rows outside the given array are not touched, a length counts as at least 0 and at most what the
- * sequence's pages hold, and a page number outside the cache makes the tokens of that page absent (not read, not written).
+ * so the kernels bound them: rows outside the given array are not touched, a length counts as at least 0 and, where the sequence is
+ * attended to, at most what its pages hold, and a page number outside the cache makes the tokens of that page absent (not read, not written).
  */
 #ifndef GQSA_ATTENTION_H
 #define GQSA_ATTENTION_H
@@ -82,7 +82,8 @@ void gqsa_cache_free(gqsa_cache_t c);
 
 /*
  * Quantise new keys and values into the cache.  The rows of sequence b become its tokens lengths[b] - n .. lengths[b] - 1 (n its
- * rows here): lengths counts the new tokens in, as gqsa_cache_attend after it wants it.  Rows that would be tokens below 0 are left out.
+ * rows here): lengths counts the new tokens in, as gqsa_cache_attend after it wants it.  Rows that would be tokens
+ * below 0, or beyond what max_pages pages hold, are left out.
  *   k, v     [device] fp16 [n_rows, kv_heads, head_dim]
  *   lengths  [device] int32 [n_seqs];  max_pages 1 .. 2^20, n_seqs 1 .. 65536
  * Two sequences of one call must not write the same page.
@@ -94,7 +95,8 @@ gqsa_status_t gqsa_cache_append(gqsa_cache_t c, const void* k, int64_t k_row_str
 
 /*
  * The values that the last tokens of each sequence stand for: row i of the n rows of sequence b is its token lengths[b] - n + i (a whole
- * sequence: n = lengths[b]).  Rows without a token (below 0, or on an absent page) are zero.
+ * sequence: n = lengths[b]).  Rows without a token (below 0, beyond the pages, or on an
+ * absent page) are zero.
  *   k_out, v_out [device] fp16 [n_rows, kv_heads, head_dim]
  */
 gqsa_status_t gqsa_cache_read(gqsa_cache_t c, void* k_out, int64_t k_row_stride, int64_t k_head_stride,

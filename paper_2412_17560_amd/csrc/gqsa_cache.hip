@@ -44,15 +44,21 @@ struct Sequence {
     int start, rows, length;       // its rows are start .. start + rows - 1, its tokens 0 .. length - 1, the last of them those of the rows
 };
 
-__device__ __forceinline__ Sequence sequence(const Sequences& s, int page_shift, int b)
+// (a length counts as at least 0 and at most `most`)
+__device__ __forceinline__ Sequence sequence(const Sequences& s, int most, int b)
 {
     const Rows rows = rows_between(s.row_starts ? s.row_starts[b] : b, s.row_starts ? s.row_starts[b + 1] : b + 1, s.n_rows);
     Sequence q;
     q.start = rows.start;
     q.rows = rows.count;
-    const int64_t most = int64_t{s.max_pages} << page_shift;
-    q.length = static_cast<int>(min(static_cast<int64_t>(max(s.lengths[b], 0)), min(most, int64_t{INT_MAX - 4096})));
+    q.length = min(max(s.lengths[b], 0), most);
     return q;
+}
+
+// What a sequence's pages hold, if they are all there.
+__device__ __forceinline__ int most_tokens(const Sequences& s, int page_shift)
+{
+    return static_cast<int>(min(int64_t{s.max_pages} << page_shift, int64_t{INT_MAX - 4096}));
 }
 
 // --------------------------------------------------------------------------- into the cache and out of it
@@ -62,7 +68,7 @@ struct CopyArgs {
     Sequences seqs;
 };
 
-// The tiles that the rows of a sequence lie in, from the first one's (which may be below 0) on.
+// The tiles that the rows of a sequence lie in, from the first one's (which may be below 0) to the last one's (which may lie beyond the pages).
 __device__ __forceinline__ int tiles_of_rows(const Sequence& q)
 {
     return q.rows == 0 ? 0 : ((q.length - 1) >> 5) - ((q.length - q.rows) >> 5) + 1;
@@ -76,7 +82,7 @@ struct Unit {
 
 __device__ __forceinline__ bool unit_of(const CopyArgs& a, Unit* u)
 {
-    const auto deal = deal_out<Sequence>(a.seqs.n_seqs, threadIdx.x & 63, [&](int s) { return sequence(a.seqs, a.pool.page_shift, s); },
+    const auto deal = deal_out<Sequence>(a.seqs.n_seqs, threadIdx.x & 63, [&](int s) { return sequence(a.seqs, INT_MAX, s); },
                                          [](const Sequence& q) { return static_cast<unsigned>(tiles_of_rows(q)); });
     if (blockIdx.x >= deal.total) return false;
     int b, within;
@@ -84,8 +90,9 @@ __device__ __forceinline__ bool unit_of(const CopyArgs& a, Unit* u)
     u->tile = ((u->seq.length - u->seq.rows) >> 5) + within;
     u->head = blockIdx.y;
     u->page = -1;
-    if (u->tile >= 0) {
-        const int page = a.seqs.pages[int64_t{b} * a.seqs.max_pages + (u->tile >> (a.pool.page_shift - 5))];
+    const int of = u->tile >> (a.pool.page_shift - 5);
+    if (of >= 0 && of < a.seqs.max_pages) {        // (a row beyond the pages is left out, not written over the last token)
+        const int page = a.seqs.pages[int64_t{b} * a.seqs.max_pages + of];
         if (page >= 0 && page < a.pool.n_pages) u->page = page;
     }
     return true;
@@ -633,7 +640,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
     const auto blocks_of = [&](const Sequence& q) { return static_cast<int>((static_cast<unsigned>(q.rows) * per + kRowBlock - 1) / kRowBlock); };
     // A step is one tile for every wavefront; or two, where there are so few that a workgroup has one or two of them: half the parts to join.
     int step_tiles = WAVES;
-    auto deal = deal_out<Sequence>(a.seqs.n_seqs, lane, [&](int b) { return sequence(a.seqs, a.pool.page_shift, b); }, [&](const Sequence& q) {
+    const int most_length = most_tokens(a.seqs, a.pool.page_shift);
+    auto deal = deal_out<Sequence>(a.seqs.n_seqs, lane, [&](int b) { return sequence(a.seqs, most_length, b); }, [&](const Sequence& q) {
         return static_cast<unsigned>(min(static_cast<int64_t>(blocks_of(q)) * steps_of(q, step_tiles) * a.pool.kv_heads, int64_t{INT_MAX}));
     });
     if (deal.total <= kFewSteps * gridDim.x) {
@@ -656,7 +664,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
         const int blocks = blocks_of(seq), steps = steps_of(seq, step_tiles);
         if (within >= blocks * steps * a.pool.kv_heads) {       // (on to the next sequence that has rows)
             within = 0;
-            seq = sequence(a.seqs, a.pool.page_shift, ++b);
+            seq = sequence(a.seqs, most_length, ++b);
             continue;
         }
         const int segment = static_cast<unsigned>(within) / static_cast<unsigned>(steps), from = within - segment * steps;

@@ -70,3 +70,27 @@ def test_starts_whose_difference_passes_32_bits_prompts(heads, q_starts, k_start
         want, size = ref.attention(q[at], kb, vb, 0.125, [len(seen) - len(rows) + i + 1 for i in range(len(rows))])
         _check_attended(out[10 + rows.start:10 + rows.stop], want, size, len(seen), vb)
     assert (out[left] == 4).all()
+
+
+# ----------------------------------------------------------------------------- sequences longer than their pages
+@pytest.mark.parametrize("dim", [64, 128])
+def test_rows_beyond_the_pages_are_left_out(dim):
+    """A sequence that outgrows its pages keeps the tokens it has, whatever is appended to it."""
+    c = Cached([60, 30], 2, dim, 32, seed=dim)                 # two pages and one: room for 64 and 32 tokens, of a table of two
+    x, y = c.some(7), c.some(7)
+    pages = dev(c.pages)
+    gq.gqsa_cache_append(c.cache, dev(x), dev(y), pages, ints(67, 30), ints(0, 7, 7))
+    c.k[0], c.v[0] = np.concatenate([c.k[0], x[:4]]), np.concatenate([c.v[0], y[:4]])
+    c.check()
+    for length in (65, 68, 96, 97, 64 + 2 ** 20, MOST - 40, MOST):
+        gq.gqsa_cache_append(c.cache, dev(x[:1]), dev(y[:1]), pages, ints(length, 30), ints(0, 1, 1))
+    gq.gqsa_cache_append(c.cache, dev(x), dev(y), pages, ints(MOST, 30), ints(0, 7, 7))
+    gq.gqsa_cache_append(c.cache, dev(x[:2]), dev(y[:2]), pages, ints(65, 100))           # a row per sequence, both beyond
+    c.check()
+    k, v = (torch.full((7, 2, dim), 3.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    gq.gqsa_cache_read(c.cache, pages, ints(67, 30), ints(0, 7, 7), k, v)       # row i: the token that append makes of it
+    for got, held in ((k, c.k[0]), (v, c.v[0])):
+        got = got.cpu().numpy()
+        assert np.array_equal(got[:4], ref.cache_values(held[60:])) and (got[4:] == 0).all()
+    gq.gqsa_cache_read(c.cache, pages, ints(MOST, 30), ints(0, 7, 7), k, v)
+    assert (k == 0).all() and (v == 0).all()
