@@ -124,7 +124,8 @@ __device__ __forceinline__ Quantised<N> quantise(const half8_t (&x)[N / 8])
     Quantised<N> q;
     q.low = bad ? static_cast<_Float16>(__builtin_nanf("")) : static_cast<_Float16>(low);
     uint16_t step_bits = __builtin_bit_cast(uint16_t, static_cast<_Float16>(bad ? 0.0f : (high - low) / 15.0f));
-    if (low + 15.0f * static_cast<float>(__builtin_bit_cast(_Float16, step_bits)) >= 65520.0f) --step_bits;       // (what rounds to infinity)
+    // (what the largest code would stand for, rounded once as it is when it is read: a sum rounded to fp32 first reaches 65520, from where on fp16 is infinity, too soon)
+    if (__builtin_fmaf16(static_cast<_Float16>(15.0f), __builtin_bit_cast(_Float16, step_bits), q.low) > static_cast<_Float16>(65504.0f)) --step_bits;
     q.step = __builtin_bit_cast(_Float16, step_bits);
     // (x - low) / step as one rounded division: with the rounded reciprocal, a product, its exact remainder and one correction.  The corrected
     // quotient is off by 2^-23 of its last place before it is rounded, and no quotient by a number of 11 bits lies that near to the middle

@@ -94,3 +94,18 @@ def test_rows_beyond_the_pages_are_left_out(dim):
         assert np.array_equal(got[:4], ref.cache_values(held[60:])) and (got[4:] == 0).all()
     gq.gqsa_cache_read(c.cache, pages, ints(MOST, 30), ints(0, 7, 7), k, v)
     assert (k == 0).all() and (v == 0).all()
+
+
+# ----------------------------------------------------------------------------- steps at the end of the range
+def test_steps_whose_largest_value_is_next_to_infinity():
+    """low + 15 step just below, at and just above where fp16 rounds to infinity: only the last two take the smaller step."""
+    c = Cached([0], 1, 64, 32, room=32)
+    x = c.some(8)
+    x[:, 0, :32] = 0
+    x[:, 0, 1] = 65504
+    x[:, 0, 2:20] = (3000 * np.arange(1, 19)).astype(np.float16)
+    for i, low in enumerate([-0.0005, -6e-8, 0, 6e-8, 0.0005, -1, -0.00195, 1]):
+        x[i, 0, 0] = low
+        x[i, 0, 20:32] = max(low, 0)
+    c.append([x], [x])
+    c.check()
