@@ -5,7 +5,8 @@
  *
  * Same conventions as gqsa.h: plain pointers and sizes, [host] or [device], a gqsa_status_t from every call, nothing thrown,
  * calls only enqueue on `hip_stream` unless said otherwise.  All activations are fp16, as x and y of the products are; sums,
- * norms and softmax statistics are fp32.
+ * norms, scores and softmax statistics are fp32.  Softmax weights are rounded to fp16 for the product with the values, and their sum is of the
+ * rounded ones: each is within 2^-11 of itself or 2^-32 of the row's largest, whichever is more.
  *
  * An array "[rows, heads, head_dim]" is given by its pointer, the distance from one row to the next and the distance from one
  * head to the next, both in elements; the elements of a head follow each other.  So a slice of a joint q/k/v array, or an array

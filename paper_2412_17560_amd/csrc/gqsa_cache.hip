@@ -344,8 +344,6 @@ struct RowState {
     float4_t out[D / 16];       // elements 16 c + 4 quad + r of row l % 16
 };
 
-constexpr float kSlack = 8.0f;      // powers of two that a score may lie above the reference before the reference follows
-
 // Of a lane's words of a tile's parameters, clears those of the tokens from `left` on, so that they stand for zero.
 template <int D>
 __device__ __forceinline__ void hide(typename Raw<D>::words_t& parameters, int lane, int left)
@@ -456,11 +454,11 @@ __device__ __forceinline__ void attend_tile(const Raw<D>& raw, uint32_t* stage, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) most = fmaxf(most, s[i >> 2][i & 3]);
     most *= scale_log2;
-    // The reference follows only where a score lies far above it: p then reaches 2^8 at most, well inside fp16.
-    if (__any(most > state.top + kSlack || (state.top == kMinusInf && most > kMinusInf))) {
+    // (the reference follows only where a score lies far above it)
+    if (__any(most > state.top + (kRoom + kSlack) || (state.top == kMinusInf && most > kMinusInf))) {
         most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
-        const float top = fmaxf(state.top, most);
+        const float top = fmaxf(state.top, most - kRoom);
         const float shrink = top == kMinusInf ? 1.0f : __builtin_amdgcn_exp2f(state.top - top);
         state.top = top;
         state.sum *= shrink;

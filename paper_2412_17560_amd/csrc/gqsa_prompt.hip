@@ -25,7 +25,6 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kWaveRows = 32;       // query rows of a wavefront
 constexpr int kTileKeys = 64;
-constexpr float kSlack = 8.0f;      // powers of two that a score may lie above its row's reference before the reference follows
 
 typedef short short4_t __attribute__((ext_vector_type(4)));
 
@@ -170,7 +169,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
     float16_t out[D / 32];
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) out[i] = float16_t{};
-    float top = kMinusInf, sum = 0.0f;
+    float top = kMinusInf, sum = 0.0f;          // the scores' reference, the weights' sum
 
     if (tiles > 0) copy(0, 0);
     for (int tile = 0; tile < tiles; ++tile) {
@@ -227,9 +226,9 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[j][r]);
         most *= c.scale;
-        if (__any(most > top + kSlack || (top == kMinusInf && most > kMinusInf))) {
+        if (__any(most > top + (kRoom + kSlack) || (top == kMinusInf && most > kMinusInf))) {
             most = fmaxf(most, __shfl_xor(most, 32));
-            const float higher = fmaxf(top, most);
+            const float higher = fmaxf(top, most - kRoom);
             const float shrink = higher == kMinusInf ? 1.0f : __builtin_amdgcn_exp2f(top - higher);
             top = higher;
             sum *= shrink;

@@ -109,3 +109,59 @@ def test_steps_whose_largest_value_is_next_to_infinity():
         x[i, 0, 20:32] = max(low, 0)
     c.append([x], [x])
     c.check()
+
+
+# ----------------------------------------------------------------------------- many small weights behind a large one
+def _sink(rng, tokens, kv_heads, q_heads, gap, of_sink, rows=1):
+    """A first token that has the weight 1, and many that lie about `gap` below it in the exponent; the first one's value is `of_sink`."""
+    q, k, v = np.zeros((rows, q_heads, 64)), np.zeros((tokens, kv_heads, 64)), 1 + 0.25 * rng.standard_normal((tokens, kv_heads, 64))
+    q[:, :, 0], k[0, :, 0], v[0] = gap / 15, 15, of_sink
+    q[:, :, 32:], k[1:, :, 32:] = rng.standard_normal((rows, q_heads, 32)), 0.05 * rng.standard_normal((tokens - 1, kv_heads, 32))
+    return [x.astype(np.float16) for x in (q, k, v)]
+
+
+def _check_sum_of_small(got, want, size, tokens, values):
+    """The largest weight is 2^7 at least, and no less is their sum.  A weight is rounded to fp16, by 2^-11 of it or by 2^-25 (2^-32 of the sum), in the product as
+    in the sum; so is the result, once (2^-11 or 2^-25); fp32 scores, exponentials and sums stay below 2^-14 of the size together."""
+    error = np.abs(got.astype(np.float64) - want)
+    bound = (3 * 2.0 ** -11 + 2.0 ** -14) * size + tokens * 2.0 ** -31 * np.abs(values).max() + 2.0 ** -25
+    assert (error <= bound).all(), (error / size).max()
+
+
+SMALL = [(131072, 17.0), (131072, 17.8), (8192, 17.8), (8192, 15.0), (1000, 14.0)]
+
+
+@pytest.mark.parametrize("of_sink", [0.0, 1.0])
+@pytest.mark.parametrize("tokens, gap", SMALL)
+def test_many_small_weights_over_the_cache(tokens, gap, of_sink):
+    c = Cached([0], 1, 64, 1024, seed=int(10 * gap), room=tokens)
+    q, k, v = _sink(c.rng, tokens, 1, 2, gap, of_sink)
+    c.append([k], [v])
+    out = gq.gqsa_cache_attend(c.cache, dev(q), dev(c.pages), ints(tokens), scale=1.0).cpu().numpy()
+    hk, hv = ref.cache_values(k), ref.cache_values(v)
+    want, size = ref.attention(q, hk, hv, 1.0, [tokens])
+    _check_sum_of_small(out, want, size, tokens, hv)
+
+
+@pytest.mark.parametrize("of_sink", [0.0, 1.0])
+@pytest.mark.parametrize("tokens, gap", [(8192, 17.8), (8192, 16.0), (30000, 17.4)])
+def test_many_small_weights_of_many_sequences_over_the_cache(tokens, gap, of_sink):
+    """As many sequences as there are workgroups, so that the large weight's wavefront has many of the small ones too; on the same pages all of them."""
+    count = 520
+    c = Cached([0], 1, 64, 1024, seed=tokens, room=tokens)
+    q, k, v = _sink(c.rng, tokens, 1, 1, gap, of_sink, rows=count)
+    c.append([k], [v])
+    pages = dev(np.repeat(c.pages, count, axis=0))
+    out = gq.gqsa_cache_attend(c.cache, dev(q), pages, ints(*[tokens] * count), scale=1.0).cpu().numpy()
+    hk, hv = ref.cache_values(k), ref.cache_values(v)
+    want, size = ref.attention(q, hk, hv, 1.0, [tokens] * count)
+    _check_sum_of_small(out, want, size, tokens, hv)
+
+
+@pytest.mark.parametrize("of_sink", [0.0, 1.0])
+@pytest.mark.parametrize("tokens, gap, heads", [*[(*s, 2) for s in SMALL], (8192, 17.8, 520), (1000, 14.0, 520)])       # rows shared by two wavefronts or not
+def test_many_small_weights_of_a_prompt(tokens, gap, heads, of_sink):
+    q, k, v = _sink(np.random.default_rng(heads), tokens, 1, heads, gap, of_sink)
+    out = gq.gqsa_prompt_attend(dev(q), dev(k), dev(v), ints(0, 1), ints(0, tokens), scale=1.0).cpu().numpy()
+    want, size = ref.attention(q, k, v, 1.0, [tokens])
+    _check_sum_of_small(out, want, size, tokens, v)
