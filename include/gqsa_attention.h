@@ -129,7 +129,8 @@ gqsa_status_t gqsa_cache_attend(gqsa_cache_t c, const void* q, int64_t q_row_str
  *   q, out   [device] fp16 [n_q_rows, q_heads, head_dim];  k, v [device] fp16 [n_k_rows, kv_heads, head_dim]
  *   head_dim 64 or 128; q_heads a multiple of kv_heads (grouped heads as in gqsa_cache_attend), at most 1024; rows of k and of v
  *            at most 2^23 elements apart (GQSA_ERR_UNSUPPORTED); (n_q_rows / 128 + n_seqs) q_heads at most 2^23 (GQSA_ERR_SHAPE)
- * Keys and values that a row does not see have no effect on it, whatever they hold.
+ * Keys and values that a row does not see have no effect on it, whatever they hold.  An infinite value that it sees makes that element of the row
+ * infinite, a NaN or infinities of both signs make it NaN, however small their weights are.
  */
 gqsa_status_t gqsa_prompt_attend(const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads, int64_t n_q_rows,
                                  const void* k, int64_t k_row_stride, int64_t k_head_stride,

@@ -111,32 +111,5 @@ __device__ __forceinline__ Deal<Seq, Load, Count> deal_out(int n_seqs, int lane,
     return {n_seqs, lane, load, count};
 }
 
-// Values that are not finite, where a mask hides some of them from some rows: a product with a weight of 0 would make them NaN for every row.  The
-// product then takes `finite_part` and a second one counts, for each row and element, the +infinities, -infinities and NaN that the row sees.
-__device__ __forceinline__ half8_t finite_part(half8_t v)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __builtin_fabsf16(v[i]) <= static_cast<_Float16>(65504.0f) ? v[i] : static_cast<_Float16>(0.0f);
-    return v;
-}
-
-__device__ __forceinline__ half8_t not_finite(half8_t v)
-{
-    half8_t m;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        m[i] = static_cast<_Float16>(__builtin_fabsf16(v[i]) <= static_cast<_Float16>(65504.0f) ? 0.0f
-                                     : v[i] != v[i] ? 16384.0f : v[i] > static_cast<_Float16>(0.0f) ? 1.0f : 128.0f);
-    return m;
-}
-
-// What those counts (of at most 64 values) add to the row's sum.
-__device__ __forceinline__ float from_counts(float count)
-{
-    const int n = static_cast<int>(count), up = n & 127, down = n >> 7 & 127;
-    if (n >= 16384 || (up && down)) return __builtin_nanf("");
-    return up ? __builtin_inff() : down ? -__builtin_inff() : 0.0f;
-}
-
 }  // namespace
 }  // namespace gqsa

@@ -63,18 +63,72 @@ __device__ __forceinline__ void copy_in(uint32_t to, uint64_t from, const uint32
                      : "+{m0}"(to) : "s"(from), "v"(at[0]), "v"(at[1]) : "memory", "scc");
 }
 
-// Whether this thread's part of a tile of values holds an infinity or a NaN.
+// Whether one of eight numbers is an infinity or a NaN: where the exponent's bits are all set, adding its lowest one carries into the sign's place.
+__device__ __forceinline__ bool some_not_finite(u32x4_t x)
+{
+    uint32_t over = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) over |= (x[e] & 0x7C007C00u) + 0x04000400u;
+    return (over & 0x80008000u) != 0;
+}
+
+// The same of this thread's part of a tile of values.
 template <int D>
 __device__ __forceinline__ bool some_not_finite(const uint16_t* tile)
 {
-    uint32_t over = 0;      // the exponent's bits all set: adding its lowest one carries into the sign's place
+    bool some = false;
 #pragma unroll
-    for (int i = 0; i < kTileKeys * D / 8 / kThreads; ++i) {
-        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(tile + (i * kThreads + threadIdx.x) * 8);
+    for (int i = 0; i < kTileKeys * D / 8 / kThreads; ++i) some |= some_not_finite(*reinterpret_cast<const u32x4_t*>(tile + (i * kThreads + threadIdx.x) * 8));
+    return some;
+}
+
+// Numbers that are not finite as 0.
+__device__ __forceinline__ half8_t finite_part(half8_t v)
+{
 #pragma unroll
-        for (int e = 0; e < 4; ++e) over |= (x[e] & 0x7C007C00u) + 0x04000400u;
+    for (int i = 0; i < 8; ++i) v[i] = __builtin_fabsf16(v[i]) <= static_cast<_Float16>(65504.0f) ? v[i] : static_cast<_Float16>(0.0f);
+    return v;
+}
+
+// Infinite values.  A row's element is infinite if the row sees one there, and NaN if it sees a NaN or both infinities, whatever the weights; but the product makes NaN of an infinity
+// whose weight is rounded to 0, and so does a rescaling by 0 later on.  So the elements that come out of the loop not finite are put together anew, by the sum of
+// the values that are not finite and that the row sees.  (Called by whole wavefronts, seldom: the wavefront goes once more through its rows' values, 64 keys at a
+// time, and looks closer at keys that hold such a value.)
+template <int D>
+__device__ __forceinline__ void sum_not_finite(const uint16_t* v, int64_t v_row, int keys, int sees, int lane, float16_t (&out)[D / 32])
+{
+    constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes;        // lanes to a key, keys to a load of 16 bytes a lane
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) out[d][r] = __builtin_fabsf(out[d][r]) < __builtin_inff() ? out[d][r] : 0.0f;
+    for (int first = 0; first < keys; first += 64) {
+        uint32_t odd = 0;           // bit i: this lane's part of key first + i kAtOnce + lane / kLanes
+        u32x4_t x[64 / kAtOnce];
+#pragma unroll
+        for (int i = 0; i < 64 / kAtOnce; ++i)
+            x[i] = *reinterpret_cast<const u32x4_t*>(v + min(first + i * kAtOnce + lane / kLanes, keys - 1) * v_row + 8 * (lane % kLanes));
+#pragma unroll
+        for (int i = 0; i < 64 / kAtOnce; ++i) odd |= (some_not_finite(x[i]) ? 1u : 0u) << i;
+        if (!__any(odd)) continue;
+        for (int i = 0; i < 64; ++i) {
+            const int key = first + i;
+            const bool mine = lane / kLanes == i % kAtOnce && (odd >> (i / kAtOnce) & 1);
+            if (key >= keys || !__any(mine)) continue;
+            const uint16_t* at = v + key * v_row + 4 * (lane >> 5);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const half4_t y = *reinterpret_cast<const half4_t*>(at + 32 * d + 8 * r);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float value = static_cast<float>(y[e]);
+                        if (key < sees && !(__builtin_fabsf(value) < __builtin_inff())) out[d][4 * r + e] += value;
+                    }
+                }
+        }
     }
-    return (over & 0x80008000u) != 0;
 }
 
 // The slot-th of the blocks of up to 64 sequences in the order of the keys they see, the most first: `level` is how many times ROWS those are, the last block of
@@ -170,6 +224,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) out[i] = float16_t{};
     float top = kMinusInf, sum = 0.0f;          // the scores' reference, the weights' sum
+    bool wild = false;
 
     if (tiles > 0) copy(0, 0);
     for (int tile = 0; tile < tiles; ++tile) {
@@ -180,38 +235,31 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
         const int mine = first + 32 * kPieces * part;          // this wavefront's first key
         const bool active = mine < wave_keys;                 // (the same for a whole wavefront)
         const uint16_t *k_tile = shared.k[buffer], *v_tile = shared.v[buffer];
-        // The two (with keys of an earlier part three) tiles that some rows see in part.  If values there are not finite, the rows that do not see them must
-        // be kept from them: see below.
-        bool wild = false;
-        if (first + kTileKeys > row0 + behind + 1) wild = __syncthreads_or(some_not_finite<D>(v_tile));
-
-        float16_t s[kPieces];
-        if (active) {
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) s[j] = float16_t{};
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-#pragma unroll
-                for (int j = 0; j < kPieces; ++j) {
-                    const int r = 32 * (kPieces * part + j) + (lane & 31);
-                    const half8_t k = *reinterpret_cast<const half8_t*>(k_tile + r * D + 8 * key_place<D>(r, 2 * i + half));
-                    s[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i], s[j], 0, 0, 0);
-                }
-            }
-        }
-        if (wild) {
-            // the keys have been read: what is not finite moves from the values' tile to the keys', as counts
-            __syncthreads();
+        // The two (with keys of an earlier part three) tiles that some rows see in part: a weight of 0 would not keep the other rows from values that are not
+        // finite.  The product takes 0 in their place; what they make of the rows that see them is seen to at the end.
+        if (first + kTileKeys > row0 + behind + 1 && __builtin_expect(__syncthreads_or(some_not_finite<D>(v_tile)), 0)) {
+            wild = true;
 #pragma unroll
             for (int i = 0; i < kTileKeys * D / 8 / kThreads; ++i) {
-                const int at = (i * kThreads + threadIdx.x) * 8;
-                const half8_t v = *reinterpret_cast<const half8_t*>(&shared.v[buffer][at]);
-                *reinterpret_cast<half8_t*>(&shared.k[buffer][at]) = not_finite(v);
-                *reinterpret_cast<half8_t*>(&shared.v[buffer][at]) = finite_part(v);
+                half8_t* at = reinterpret_cast<half8_t*>(&shared.v[buffer][(i * kThreads + threadIdx.x) * 8]);
+                *at = finite_part(*at);
             }
             __syncthreads();
         }
         if (!active) continue;
+
+        float16_t s[kPieces];
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) s[j] = float16_t{};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int r = 32 * (kPieces * part + j) + (lane & 31);
+                const half8_t k = *reinterpret_cast<const half8_t*>(k_tile + r * D + 8 * key_place<D>(r, 2 * i + half));
+                s[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i], s[j], 0, 0, 0);
+            }
+        }
         // element r of s[j] is key 32 j + r % 4 + 8 (r / 4) + 4 half of the wavefront's
         if (mine + 32 * kPieces > wave_row0 + behind + 1) {
 #pragma unroll
@@ -266,22 +314,6 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(turned(v_tile, 2 * kPieces * part + i, d), p[i], out[d], 0, 0, 0);
         __builtin_amdgcn_s_setprio(0);
-        if (wild) {
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d) {
-                float16_t count = float16_t{};
-#pragma unroll
-                for (int i = 0; i < 2 * kPieces; ++i) {
-                    half8_t seen;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) seen[e] = static_cast<_Float16>(mine + 16 * i + 8 * (e >> 2) + 4 * half + (e & 3) < sees ? 1.0f : 0.0f);
-                    count = __builtin_amdgcn_mfma_f32_32x32x16_f16(turned(k_tile, 2 * kPieces * part + i, d), seen, count, 0, 0, 0);
-                }
-#pragma unroll
-                for (int r = 0; r < 16; ++r) out[d][r] += from_counts(count[r]);
-                __builtin_amdgcn_sched_barrier(0);      // (one after the other: few registers, not speed)
-            }
-        }
     }
 
     sum += __shfl_xor(sum, 32);
@@ -310,8 +342,17 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
     int own_lane = lane;
     asm volatile("" : "+v"(own_lane));
     const int own_row = wave_row0 + (own_lane & 31);
+    // (a row whose sum is not finite is NaN throughout)
+    float largest_out = 0.0f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) largest_out = __builtin_elementwise_maximum(largest_out, __builtin_fabsf(out[d][r]));
+    if (__builtin_expect(wild || __any(!(largest_out < __builtin_inff()) && sum < __builtin_inff()), 0))
+        sum_not_finite<D>(reinterpret_cast<const uint16_t*>(v_from), c.v.row, wave_keys, own_row + behind + 1, own_lane, out);
     if (own_row >= n_q) return;
-    const float inverse = own_row + behind >= 0 ? 1.0f / sum : 0.0f;       // (a row without keys: all sums are 0; one with scores of -infinity only is NaN)
+    // (a row without keys: all sums are 0; one with scores of -infinity only is NaN)
+    const float inverse = own_row + behind < 0 ? 0.0f : sum == 0.0f ? __builtin_nanf("") : 1.0f / sum;
     uint16_t* to = c.out.data + (int64_t{q_start} + own_row) * c.out.row + head * c.out.head + 4 * (own_lane >> 5);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)

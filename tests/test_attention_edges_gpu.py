@@ -6,7 +6,7 @@ import pytest
 
 import paper_2412_17560_amd as gq
 from oracle import attention as ref
-from test_attention_gpu import Cached, _check_attended, dev, ints, normal
+from test_attention_gpu import Cached, _check_attended, _check_prompts, dev, ints, normal
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -165,3 +165,34 @@ def test_many_small_weights_of_a_prompt(tokens, gap, heads, of_sink):
     out = gq.gqsa_prompt_attend(dev(q), dev(k), dev(v), ints(0, 1), ints(0, tokens), scale=1.0).cpu().numpy()
     want, size = ref.attention(q, k, v, 1.0, [tokens])
     _check_sum_of_small(out, want, size, tokens, v)
+
+
+# ----------------------------------------------------------------------------- infinite values
+@pytest.mark.parametrize("heads", [2, 96])          # rows shared by two wavefronts or not
+@pytest.mark.parametrize("dim", [64, 128])
+def test_infinite_values_of_any_weight(dim, heads):
+    """An infinite value that a row sees makes the element infinite and a NaN, or two infinities of different signs, make it NaN, even where the weight is far below
+    what 32 bits hold, wherever the key lies among those that the row sees."""
+    rng = np.random.default_rng(dim)
+    rows = 400
+    q, k, v = normal(rng, rows, heads, dim), normal(rng, rows, 1, dim), normal(rng, rows, 1, dim)
+    q[:, :, 0], k[:, :, 0] = 8, 0
+    low = [3, 70, 71, 200, 390]
+    k[low, :, 0] = -400                                        # scores of -3200 and less
+    k[low, :, 1:] = 0
+    v[3, 0, 5], v[70, 0, 6], v[71, 0, 6], v[70, 0, 7], v[71, 0, 7] = np.inf, -np.inf, -np.inf, np.inf, -np.inf
+    v[200, 0, 8], v[390, 0, 9], v[390, 0, 10] = np.nan, -np.inf, np.inf
+    v[100, 0, 11] = -np.inf                                    # (of a weight like the others')
+    starts = ints(0, rows)
+    out = gq.gqsa_prompt_attend(dev(q), dev(k), dev(v), starts, starts, scale=1.0).cpu().numpy()
+    special = np.zeros(out.shape, bool)
+    for element, first, value in [(5, 3, np.inf), (6, 70, -np.inf), (7, 71, np.nan), (8, 200, np.nan), (9, 390, -np.inf), (10, 390, np.inf), (11, 100, -np.inf)]:
+        special[first:, :, element] = True
+        assert np.array_equal(out[first:, :, element], np.full((rows - first, heads), value), equal_nan=True), element
+    assert (out[70, :, 7] == np.inf).all()
+    special[70, :, 7] = True
+    finite = np.where(np.isfinite(v), v, 0)
+    want = gq.gqsa_prompt_attend(dev(q), dev(k), dev(finite), starts, starts, scale=1.0).cpu().numpy()
+    assert np.array_equal(out[~special], want[~special])
+    heads_checked = slice(0, 2)
+    _check_prompts(want[:, heads_checked], q[:, heads_checked], k, finite, [0, rows], [0, rows], 1.0)
