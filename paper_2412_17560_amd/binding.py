@@ -328,11 +328,12 @@ def _torch():
     return torch
 
 
-def _stream_ptr(stream):
+def _stream_ptr(stream, device=None):
+    """(device: the current one's number, where the caller has it)"""
     if stream is None:
         torch = _TORCH or _torch()
         try:                 # (not public names, but torch.cuda.current_stream() makes an object a call)
-            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice() if device is None else device)
         except AttributeError:
             return torch.cuda.current_stream().cuda_stream
     return C.c_void_p(getattr(stream, "cuda_stream", stream))      # (an integer; as an argument itself ctypes would take a text too)
@@ -476,34 +477,53 @@ def _names():
     _HALF, _INT, _FLOAT = torch.float16, torch.int32, torch.float32
 
 
-def _heads(t, what: str):
-    """(pointer, distance between rows, distance between heads, rows, heads, head_dim) of a float16 device tensor [rows, heads, head_dim]
+def _device_of(t) -> int:
+    """Number of the device of a call's first tensor, where the others have to lie too, and which has to be the current one: the launch goes there, and nothing else would
+    notice.  -2 for what is on no device, or no tensor: nothing lies there."""
+    try:
+        device = t.get_device()
+    except AttributeError:
+        return -2
+    if device < 0:
+        return -2
+    torch = _TORCH or _torch()
+    try:                 # (as in _stream_ptr)
+        current = torch._C._cuda_getDevice()
+    except AttributeError:
+        current = torch.cuda.current_device()
+    if device != current:
+        raise ValueError(f"tensors on device {device}, but the current device is {current}")
+    return device
+
+
+def _heads(t, what: str, device: int):
+    """(pointer, distance between rows, distance between heads, rows, heads, head_dim) of a float16 tensor [rows, heads, head_dim] on that device
     whose heads are contiguous; the other two dimensions may be strided."""
     if _HALF is None:
         _names()
     try:
         rows, heads, dim = t.shape
         row, head, one = t.stride()
-        if (one == 1 or rows == 0) and t.dtype is _HALF and t.is_cuda:
+        if (one == 1 or rows == 0) and t.dtype is _HALF and t.get_device() == device:
             # (torch lets the distance of a dimension of size 1 be anything, and all of them without rows)
             return t.data_ptr(), row if rows > 1 else 0, head if heads > 1 else 0, rows, heads, dim
     except (AttributeError, TypeError, ValueError):
         pass
-    raise ValueError(f"{what} must be a float16 device tensor [rows, heads, head_dim] with contiguous heads")
+    raise ValueError(f"{what} must be a float16 device tensor [rows, heads, head_dim] with contiguous heads, on the device of the others")
 
 
-def _heads_like(t, what: str, rows: int, heads: int, dim: int):
+def _heads_like(t, what: str, rows: int, heads: int, dim: int, device: int):
     """The first three of _heads, of an array of that shape."""
-    at, row, head, t_rows, t_heads, t_dim = _heads(t, what)
+    at, row, head, t_rows, t_heads, t_dim = _heads(t, what, device)
     if t_rows != rows or t_heads != heads or t_dim != dim:
         raise ValueError(f"{what} must be [{rows}, {heads}, {dim}]")
     return at, row, head
 
 
-def _flat(t, dtype, what: str):
-    """(pointer, shape) of a contiguous device tensor of that dtype."""
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} device tensor")
+def _flat(t, dtype, what: str, device: int):
+    """(pointer, shape) of a contiguous tensor of that dtype on that device."""
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} device tensor, on the device of the others")
     return t.data_ptr(), t.shape
 
 
@@ -518,8 +538,8 @@ def _like(x, stream):
         return torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
-def _norm_weight(w, dim: int):
-    at, shape = _flat(w, _HALF, "norm weights")
+def _norm_weight(w, dim: int, device: int):
+    at, shape = _flat(w, _HALF, "norm weights", device)
     if len(shape) != 1 or shape[0] != dim:
         raise ValueError("norm weights must be [head_dim]")
     return at
@@ -530,34 +550,35 @@ def gqsa_qk_norm_rotate(q, k, positions, table, q_weight=None, k_weight=None, ep
     """Norms of queries [rows, q_heads, head_dim] and keys [rows, k_heads, head_dim] per head (weights float16 [head_dim] or None: no norm)
     and their rotation: positions int32 [rows], table float32 [n_positions, rotary_dim / 2, 2] (cosine, sine), or both None: no
     rotation.  k None: queries only.  q_out = q, k_out = k: in place.  Returns (q_out, k_out)."""
-    q_at, q_row, q_head, rows, q_heads, dim = _heads(q, "q")
+    device = _device_of(q)
+    q_at, q_row, q_head, rows, q_heads, dim = _heads(q, "q", device)
     if q_out is None:
         q_out = _like(q, stream)
-    qo_at, qo_row, qo_head = _heads_like(q_out, "q_out", rows, q_heads, dim)
+    qo_at, qo_row, qo_head = _heads_like(q_out, "q_out", rows, q_heads, dim, device)
     k_at, k_row, k_head, k_heads, ko_at, ko_row, ko_head = None, 0, 0, 0, None, 0, 0
     if k is not None:
-        k_at, k_row, k_head, k_rows, k_heads, k_dim = _heads(k, "k")
+        k_at, k_row, k_head, k_rows, k_heads, k_dim = _heads(k, "k", device)
         if k_out is None:
             k_out = _like(k, stream)
         if k_rows != rows or k_dim != dim:
             raise ValueError("k must be [rows, k_heads, head_dim]")
-        ko_at, ko_row, ko_head = _heads_like(k_out, "k_out", rows, k_heads, dim)
+        ko_at, ko_row, ko_head = _heads_like(k_out, "k_out", rows, k_heads, dim, device)
     n_positions = rotary = 0
     table_at = positions_at = None
     if table is not None:
-        table_at, shape = _flat(table, _FLOAT, "table")
+        table_at, shape = _flat(table, _FLOAT, "table", device)
         n_positions, half, two = shape if len(shape) == 3 else (0, 0, 0)
         if two != 2 or positions is None:
             raise ValueError("table must be [n_positions, rotary_dim / 2, 2] and positions [rows]")
-        positions_at, shape = _flat(positions, _INT, "positions")
+        positions_at, shape = _flat(positions, _INT, "positions", device)
         if len(shape) != 1 or shape[0] != rows:
             raise ValueError("positions must be [rows]")
         rotary = 2 * half
-    q_weight_at = None if q_weight is None else _norm_weight(q_weight, dim)
-    k_weight_at = None if k_weight is None else _norm_weight(k_weight, dim)
+    q_weight_at = None if q_weight is None else _norm_weight(q_weight, dim, device)
+    k_weight_at = None if k_weight is None else _norm_weight(k_weight, dim, device)
     _check(_lib().gqsa_qk_norm_rotate(
         q_at, q_row, q_head, q_heads, k_at, k_row, k_head, k_heads, rows, dim, q_weight_at, k_weight_at, eps, table_at,
-        n_positions, rotary, interleaved, positions_at, qo_at, qo_row, qo_head, ko_at, ko_row, ko_head, _stream_ptr(stream)), "gqsa_qk_norm_rotate")
+        n_positions, rotary, interleaved, positions_at, qo_at, qo_row, qo_head, ko_at, ko_row, ko_head, _stream_ptr(stream, device)), "gqsa_qk_norm_rotate")
     return q_out, k_out
 
 
@@ -594,53 +615,56 @@ def gqsa_cache_free(c: GqsaCache) -> None:
         c.ptr = C.c_void_p()
 
 
-def _sequences(pages, lengths, row_starts):
+def _sequences(pages, lengths, row_starts, device: int):
     """pages int32 [n_seqs, max_pages], lengths int32 [n_seqs], row_starts int32 [n_seqs + 1] or None (a row per sequence)."""
-    pages_at, shape = _flat(pages, _INT, "pages")
-    lengths_at, n_lengths = _flat(lengths, _INT, "lengths")
+    pages_at, shape = _flat(pages, _INT, "pages", device)
+    lengths_at, n_lengths = _flat(lengths, _INT, "lengths", device)
     if len(shape) != 2 or len(n_lengths) != 1 or n_lengths[0] != shape[0]:
         raise ValueError("pages must be [n_seqs, max_pages] and lengths [n_seqs]")
     n, max_pages = shape
     starts_at = None
     if row_starts is not None:
-        starts_at, shape = _flat(row_starts, _INT, "row_starts")
+        starts_at, shape = _flat(row_starts, _INT, "row_starts", device)
         if len(shape) != 1 or shape[0] != n + 1:
             raise ValueError("row_starts must be [n_seqs + 1]")
     return pages_at, max_pages, lengths_at, starts_at, n
 
 
-def _cache_rows(c: GqsaCache, k, v, k_what: str, v_what: str):
+def _cache_rows(c: GqsaCache, k, v, k_what: str, v_what: str, device: int):
     """Pointers and distances of keys and values of the cache's heads, and their rows."""
-    k_at, k_row, k_head, rows, heads, dim = _heads(k, k_what)
+    k_at, k_row, k_head, rows, heads, dim = _heads(k, k_what, device)
     if heads != c.kv_heads or dim != c.head_dim:
         raise ValueError("keys and values must be [rows, kv_heads, head_dim] of the cache")
-    v_at, v_row, v_head = _heads_like(v, v_what, rows, heads, dim)
+    v_at, v_row, v_head = _heads_like(v, v_what, rows, heads, dim, device)
     return k_at, k_row, k_head, v_at, v_row, v_head, rows
 
 
 def gqsa_cache_append(c: GqsaCache, k, v, pages, lengths, row_starts=None, stream=None) -> None:
     """New keys and values [rows, kv_heads, head_dim] become the last tokens of their sequences; lengths counts them in."""
-    _check(_lib().gqsa_cache_append(c.ptr, *_cache_rows(c, k, v, "k", "v"), *_sequences(pages, lengths, row_starts), _stream_ptr(stream)),
-           "gqsa_cache_append")
+    device = _device_of(k)
+    _check(_lib().gqsa_cache_append(c.ptr, *_cache_rows(c, k, v, "k", "v", device), *_sequences(pages, lengths, row_starts, device),
+                                    _stream_ptr(stream, device)), "gqsa_cache_append")
 
 
 def gqsa_cache_read(c: GqsaCache, pages, lengths, row_starts, k_out, v_out, stream=None):
     """The values of the last tokens of each sequence, as many as it has rows in k_out and v_out [rows, kv_heads, head_dim]."""
-    _check(_lib().gqsa_cache_read(c.ptr, *_cache_rows(c, k_out, v_out, "k_out", "v_out"), *_sequences(pages, lengths, row_starts),
-                                  _stream_ptr(stream)), "gqsa_cache_read")
+    device = _device_of(k_out)
+    _check(_lib().gqsa_cache_read(c.ptr, *_cache_rows(c, k_out, v_out, "k_out", "v_out", device), *_sequences(pages, lengths, row_starts, device),
+                                  _stream_ptr(stream, device)), "gqsa_cache_read")
     return k_out, v_out
 
 
 def gqsa_cache_attend(c: GqsaCache, q, pages, lengths, row_starts=None, scale: float = None, out=None, stream=None):
     """Attention of the newest rows q [rows, q_heads, head_dim] of each sequence over its cache; scale None: head_dim ** -0.5."""
-    q_at, q_row, q_head, rows, heads, dim = _heads(q, "q")
+    device = _device_of(q)
+    q_at, q_row, q_head, rows, heads, dim = _heads(q, "q", device)
     if dim != c.head_dim:
         raise ValueError("q must be [rows, q_heads, head_dim] of the cache")
     if out is None:
         out = _like(q, stream)
-    out_at, out_row, out_head = _heads_like(out, "out", rows, heads, dim)
-    _check(_lib().gqsa_cache_attend(c.ptr, q_at, q_row, q_head, heads, rows, *_sequences(pages, lengths, row_starts),
-                                    dim ** -0.5 if scale is None else scale, out_at, out_row, out_head, _stream_ptr(stream)),
+    out_at, out_row, out_head = _heads_like(out, "out", rows, heads, dim, device)
+    _check(_lib().gqsa_cache_attend(c.ptr, q_at, q_row, q_head, heads, rows, *_sequences(pages, lengths, row_starts, device),
+                                    dim ** -0.5 if scale is None else scale, out_at, out_row, out_head, _stream_ptr(stream, device)),
            "gqsa_cache_attend")
     return out
 
@@ -648,19 +672,20 @@ def gqsa_cache_attend(c: GqsaCache, q, pages, lengths, row_starts=None, scale: f
 def gqsa_prompt_attend(q, k, v, q_starts, k_starts, scale: float = None, out=None, stream=None):
     """Causal attention over packed prompts: q [q_rows, q_heads, head_dim], k and v [k_rows, kv_heads, head_dim], starts int32
     [n_seqs + 1] of each sequence's rows; scale None: head_dim ** -0.5."""
-    q_at, q_row, q_head, rows, heads, dim = _heads(q, "q")
-    k_at, k_row, k_head, k_rows, kv_heads, k_dim = _heads(k, "k")
+    device = _device_of(q)
+    q_at, q_row, q_head, rows, heads, dim = _heads(q, "q", device)
+    k_at, k_row, k_head, k_rows, kv_heads, k_dim = _heads(k, "k", device)
     if k_dim != dim:
         raise ValueError("k and v must be [k_rows, kv_heads, head_dim]")
-    v_at, v_row, v_head = _heads_like(v, "v", k_rows, kv_heads, dim)
-    q_starts_at, n_starts = _flat(q_starts, _INT, "q_starts")
-    k_starts_at, shape = _flat(k_starts, _INT, "k_starts")
+    v_at, v_row, v_head = _heads_like(v, "v", k_rows, kv_heads, dim, device)
+    q_starts_at, n_starts = _flat(q_starts, _INT, "q_starts", device)
+    k_starts_at, shape = _flat(k_starts, _INT, "k_starts", device)
     if len(n_starts) != 1 or shape != n_starts:
         raise ValueError("q_starts and k_starts must be [n_seqs + 1]")
     if out is None:
         out = _like(q, stream)
-    out_at, out_row, out_head = _heads_like(out, "out", rows, heads, dim)
+    out_at, out_row, out_head = _heads_like(out, "out", rows, heads, dim, device)
     _check(_lib().gqsa_prompt_attend(q_at, q_row, q_head, heads, rows, k_at, k_row, k_head, v_at, v_row, v_head, kv_heads, k_rows, dim,
                                      q_starts_at, k_starts_at, n_starts[0] - 1, dim ** -0.5 if scale is None else scale,
-                                     out_at, out_row, out_head, _stream_ptr(stream)), "gqsa_prompt_attend")
+                                     out_at, out_row, out_head, _stream_ptr(stream, device)), "gqsa_prompt_attend")
     return out
