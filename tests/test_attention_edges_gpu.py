@@ -196,3 +196,14 @@ def test_infinite_values_of_any_weight(dim, heads):
     assert np.array_equal(out[~special], want[~special])
     heads_checked = slice(0, 2)
     _check_prompts(want[:, heads_checked], q[:, heads_checked], k, finite, [0, rows], [0, rows], 1.0)
+
+
+# ----------------------------------------------------------------------------- the example
+@pytest.mark.parametrize("tokens, prompts", [(1, "64,3"), (2, "63,64")])
+def test_example_command_with_few_tokens(monkeypatch, capsys, tokens, prompts):
+    from paper_2412_17560_amd import attention_layer
+    monkeypatch.setattr("sys.argv", ["attention_layer", "--hidden", "512", "--heads", "8", "--kv-heads", "2", "--head-dim", "64",
+                                     "--prompts", prompts, "--tokens", str(tokens)])
+    attention_layer.main()
+    printed = capsys.readouterr().out
+    assert "prompts of" in printed and "cache" in printed and ("us a step" in printed) == (tokens > 1)
