@@ -51,7 +51,7 @@ class AttentionLayer:
         q, k, v = self._queries_keys_values(x, positions)
         gq.gqsa_cache_append(self.cache, k, v, pages, lengths, starts)
         attended = gq.gqsa_prompt_attend(q, k, v, starts, starts)
-        return self._products([self.o], attended.view(x.shape[0], -1))[0]
+        return self._products([self.o], attended.view(x.shape[0], self.heads * self.head_dim))[0]
 
     def step(self, x, positions, pages, lengths):
         """One new row for every sequence; lengths counts it in."""
@@ -59,7 +59,7 @@ class AttentionLayer:
         q, k, v = self._queries_keys_values(x, positions)
         gq.gqsa_cache_append(self.cache, k, v, pages, lengths)
         attended = gq.gqsa_cache_attend(self.cache, q, pages, lengths)
-        return self._products([self.o], attended.view(x.shape[0], -1))[0]
+        return self._products([self.o], attended.view(x.shape[0], self.heads * self.head_dim))[0]
 
 
 def rotary_table(positions: int, rotary_dim: int, theta: float = 10000.0):

@@ -207,3 +207,15 @@ def test_example_command_with_few_tokens(monkeypatch, capsys, tokens, prompts):
     attention_layer.main()
     printed = capsys.readouterr().out
     assert "prompts of" in printed and "cache" in printed and ("us a step" in printed) == (tokens > 1)
+
+
+def test_a_layer_without_rows():
+    import gqsa_inputs as gi
+    from paper_2412_17560_amd.attention_layer import AttentionLayer, rotary_table
+
+    hidden, heads, kv_heads, dim = 256, 4, 2, 64
+    sizes = [(heads * dim, hidden), (kv_heads * dim, hidden), (kv_heads * dim, hidden), (hidden, heads * dim)]
+    c = Cached([0, 0], kv_heads, dim, 32, room=64)
+    layer = AttentionLayer(*[gq.gqsa_pack(gi.dense_weight(n, k, seed=i), 16, 4, 0.5) for i, (n, k) in enumerate(sizes)], heads, rotary_table(64, dim), c.cache)
+    x = torch.empty((0, hidden), dtype=torch.float16, device="cuda")
+    assert layer.prompt(x, ints(), dev(c.pages), ints(0, 0, 0), ints(0, 0)).shape == (0, hidden)
