@@ -6,7 +6,7 @@ import pytest
 
 import paper_2412_17560_amd as gq
 from oracle import attention as ref
-from test_attention_gpu import Cached, _check_attended, _check_prompts, dev, ints, normal
+from test_attention_gpu import Cached, _check_attended, _check_prompts, _check_rotated, dev, ints, normal
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -219,3 +219,53 @@ def test_a_layer_without_rows():
     layer = AttentionLayer(*[gq.gqsa_pack(gi.dense_weight(n, k, seed=i), 16, 4, 0.5) for i, (n, k) in enumerate(sizes)], heads, rotary_table(64, dim), c.cache)
     x = torch.empty((0, hidden), dtype=torch.float16, device="cuda")
     assert layer.prompt(x, ints(), dev(c.pages), ints(0, 0, 0), ints(0, 0)).shape == (0, hidden)
+
+
+# ----------------------------------------------------------------------------- more than 64 sequences, and the queries of a layer
+@pytest.mark.parametrize("dim, q_heads, kv_heads, count, least", [
+    (64, 4, 2, 130, 1), (128, 1, 1, 65, 1), (64, 24, 8, 200, 1),
+    (64, 8, 2, 75, 130)])                                      # as long as those whose blocks are mixed, but for their number
+def test_prompts_of_many_sequences(dim, q_heads, kv_heads, count, least):
+    """More sequences than a wavefront has lanes, some without rows, some without keys, some with an earlier part."""
+    rng = np.random.default_rng(count)
+    q_rows = [0 if b % 7 == 3 else least + (29 * b) % 70 for b in range(count)]
+    q_rows[64] = 150
+    k_rows = [0 if b % 11 == 5 else n + (b % 3) * 20 for b, n in enumerate(q_rows)]
+    q, k, v = normal(rng, sum(q_rows), q_heads, dim), normal(rng, sum(k_rows), kv_heads, dim), normal(rng, sum(k_rows), kv_heads, dim)
+    qs, ks = (np.cumsum([0] + n).astype(np.int32) for n in (q_rows, k_rows))
+    out = torch.full(q.shape, 9.0, dtype=torch.float16, device="cuda")
+    gq.gqsa_prompt_attend(dev(q), dev(k), dev(v), dev(qs), dev(ks), out=out)
+    _check_prompts(out.cpu().numpy(), q, k, v, qs, ks, dim ** -0.5)
+
+
+def test_queries_that_a_layer_attends_with():
+    """What both attentions get are the normed and rotated queries, of the rows' own positions, with the queries' own weights."""
+    import gqsa_inputs as gi
+    from paper_2412_17560_amd.attention_layer import AttentionLayer, rotary_table
+
+    hidden, heads, kv_heads, dim, counts = 256, 4, 2, 64, [37, 5]
+    sizes = [(heads * dim, hidden), (kv_heads * dim, hidden), (kv_heads * dim, hidden), (hidden, heads * dim)]
+    c = Cached([0, 0], kv_heads, dim, 32, room=64)
+    norms = [normal(c.rng, dim) for _ in range(2)]
+    table = rotary_table(64, dim)
+    layer = AttentionLayer(*[gq.gqsa_pack(gi.dense_weight(n, k, seed=i), 16, 4, 0.5) for i, (n, k) in enumerate(sizes)], heads, table, c.cache,
+                           *map(dev, norms))
+    starts = np.cumsum([0] + counts).astype(np.int32)
+    positions = np.concatenate([np.arange(n) for n in counts]).astype(np.int32)
+    seen = []
+
+    def watch(original, place):
+        def call(*args, **kw):
+            seen.append(args[place].cpu().numpy().copy())
+            return original(*args, **kw)
+        return call
+
+    with pytest.MonkeyPatch.context() as m:
+        for name, place in (("gqsa_qk_norm_rotate", 0), ("gqsa_prompt_attend", 0), ("gqsa_cache_attend", 1)):
+            m.setattr(gq, name, watch(getattr(gq, name), place))
+        layer.prompt(dev(normal(c.rng, sum(counts), hidden)), dev(positions), dev(c.pages), dev(starts), ints(*counts))
+        layer.step(dev(normal(c.rng, 2, hidden)), ints(*counts), dev(c.pages), ints(*(n + 1 for n in counts)))
+    assert len(seen) == 4
+    for raw, turned, where in ((seen[0], seen[1], positions), (seen[2], seen[3], np.array(counts))):
+        assert np.abs(raw).max() > 0
+        _check_rotated(turned, raw, positions=where, table=table.cpu().numpy(), weight=norms[0])
