@@ -3,20 +3,22 @@
  * keys of each head with the rotation by position, a paged cache of keys and values in 4 bits, attention of the newest tokens
  * over that cache (token generation), and causal attention over packed prompts.
  *
- * Same conventions as gqsa.h: plain pointers and sizes, [host] or [device], a gqsa_status_t from every call, nothing thrown,
- * calls only enqueue on `hip_stream` unless said otherwise.  All activations are fp16, as x and y of the products are; sums,
- * norms, scores and softmax statistics are fp32.  Softmax weights are rounded to fp16 for the product with the values, and their sum is of the
- * rounded ones: each is within 2^-11 of itself or 2^-32 of the row's largest, whichever is more.
+ * Same conventions as gqsa.h: plain pointers and sizes, [host] or [device], a gqsa_status_t from every call, nothing thrown.
+ * Calls only enqueue on `hip_stream` unless said otherwise: a stream of the current HIP device, where all [device] arrays lie.  All
+ * activations are fp16, as x and y of the products are; sums, norms, scores and softmax statistics are fp32.  Softmax weights are
+ * rounded to fp16 for the product with the values, and their sum is of the rounded ones: each is within 2^-11 of itself or 2^-32 of
+ * the row's largest, whichever is more.
  *
  * An array "[rows, heads, head_dim]" is given by its pointer, the distance from one row to the next and the distance from one
  * head to the next, both in elements; the elements of a head follow each other.  So a slice of a joint q/k/v array, or an array
  * with the heads outermost, is taken as it is.  Pointers must be 16-byte aligned and distances multiples of 8 (GQSA_ERR_ALIGN)
- * and not negative (GQSA_ERR_SHAPE).  A call with no rows does nothing, whatever its pointers.  At most 2^25 rows.
+ * and not negative (GQSA_ERR_SHAPE).  Results must not overlap what a call reads, unless it says that they may.  A call with no
+ * rows does nothing, whatever its pointers.  At most 2^25 rows.
  *
  * Several sequences lie one behind the other in the rows: sequence b has the rows row_starts[b] .. row_starts[b + 1] - 1
  * (row_starts [device] int32[n_seqs + 1], or NULL: one row per sequence).  Values on the device cannot be refused by the host,
- * so the kernels bound them: rows outside the given array are not touched, a length counts as at least 0 and, where the sequence is
- * attended to, at most what its pages hold, and a page number outside the cache makes the tokens of that page absent (not read, not written).
+ * so the kernels bound them: rows outside the given array are not touched, a length counts as at least 0 and, in attention, at most
+ * what the sequence's pages hold, and a page number outside the cache makes the tokens of that page absent (not read, not written).
  */
 #ifndef GQSA_ATTENTION_H
 #define GQSA_ATTENTION_H
@@ -83,8 +85,8 @@ void gqsa_cache_free(gqsa_cache_t c);
 
 /*
  * Quantise new keys and values into the cache.  The rows of sequence b become its tokens lengths[b] - n .. lengths[b] - 1 (n its
- * rows here): lengths counts the new tokens in, as gqsa_cache_attend after it wants it.  Rows that would be tokens
- * below 0, or beyond what max_pages pages hold, are left out.
+ * rows here): lengths counts the new tokens in, as gqsa_cache_attend after it wants it.  Rows that would be tokens below 0, or
+ * beyond what max_pages pages hold, are left out.
  *   k, v     [device] fp16 [n_rows, kv_heads, head_dim]
  *   lengths  [device] int32 [n_seqs];  max_pages 1 .. 2^20, n_seqs 1 .. 65536
  * Two sequences of one call must not write the same page.
@@ -96,8 +98,7 @@ gqsa_status_t gqsa_cache_append(gqsa_cache_t c, const void* k, int64_t k_row_str
 
 /*
  * The values that the last tokens of each sequence stand for: row i of the n rows of sequence b is its token lengths[b] - n + i (a whole
- * sequence: n = lengths[b]).  Rows without a token (below 0, beyond the pages, or on an
- * absent page) are zero.
+ * sequence: n = lengths[b]).  Rows without a token (below 0, beyond the pages, or on an absent page) are zero.
  *   k_out, v_out [device] fp16 [n_rows, kv_heads, head_dim]
  */
 gqsa_status_t gqsa_cache_read(gqsa_cache_t c, void* k_out, int64_t k_row_stride, int64_t k_head_stride,

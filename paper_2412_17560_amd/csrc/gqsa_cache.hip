@@ -144,8 +144,9 @@ __device__ __forceinline__ Quantised<N> quantise(const half8_t (&x)[N / 8])
 // One workgroup per tile that gets rows, and head: 8 threads to a token.  The tile is put together in LDS -- a word of key codes is of one token, but one of
 // value codes of 8 -- and written in runs of 16 bytes; of a tile that keeps earlier tokens, only the new ones' words and halves are
 // written, and words of value codes that they share are read first (nobody else writes the tile).
-// Few tokens are a chain of waits (lengths and starts, the page's number, the rows, LDS): 1 token of 16 sequences and 32 heads takes 4.8 us, where an empty launch
-// takes 1.6.  Many are bound by that chain and by the arithmetic of 32 codes a thread: 8192 tokens of 8 heads of 128 take 16 us, 44 MB at 2.8 TB/s.
+// Few tokens are a chain of waits: lengths and starts, the page's number, the rows (asked for only when the page is known to be there, though they do not depend on it), then
+// LDS, the bytes of a word of value codes one after the other, each waited for.  1 token of 16 sequences and 8 heads takes 5.1 us, where an empty launch takes 1.6.  Many
+// are bound by that chain and by the arithmetic of 32 codes a thread: 8192 tokens of 8 heads of 128 take 15 to 16 us, 44 MB at 2.8 TB/s; their bytes alone would take 8.5.
 template <int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(CopyArgs a)
 {
@@ -167,7 +168,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CopyArgs a)
     uint32_t old[kWords] = {};
     if (!all) {
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) {              // (whether wanted or not: ahead of everything else)
+        // (Whether wanted or not, ahead of everything else, and with one store under one condition below.  Loaded only where a word is shared, in branches of three
+        // ways with a store in two of them, the heads of 64 were compiled to a store whose 64-bit address had its upper half set on two of the ways only, and faulted.)
+        for (int i = 0; i < kWords; ++i) {
             const int at = i * kThreads + threadIdx.x;
             old[i] = *reinterpret_cast<const uint32_t*>(tile + 16 * D + word_offset(at >> 6, at & 63));
         }
@@ -241,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CopyArgs a)
 }
 
 // The same deal.  A tile comes into LDS in runs of 16 bytes, as the codes of a token are spread over words of other tokens; bound by the same chain: 8192 tokens of
-// 8 heads of 128 take 13 us (3.4 TB/s), 1 of 16 sequences and 32 heads 3.4.
+// 8 heads of 128 take 11 to 12 us (3.8 TB/s), 1 of 16 sequences and 8 heads 3.3.
 template <int D>
 __global__ __launch_bounds__(kThreads) void read_kernel(CopyArgs a)
 {
@@ -618,13 +621,13 @@ constexpr unsigned kFewSteps = 2;
 // workgroup takes a run, all of one length or one more.  Where a segment (one block of rows of one head) lies in several workgroups, each
 // leaves its maximum, sum and weighted sum in the workspace, and the last to arrive joins them in the order of the tokens.
 //
-// One row for a head of the cache is bound by memory: 16 x 4096 tokens of 32 heads of 128, 336 MB, take 65.5 us, 5.1 TB/s; the same with all tiles in the L2 caches
-// 49 us, which is what the vector instructions take (88 of them turn a tile's 1024 words of keys into numbers, 88 the values; a softmax of 16 x 32 scores 60; 16
-// products).  Several rows for a head hide nothing more: up to 16 cost what one costs, and every further 16 the instructions anew: 8 ragged sequences of up to 16003
-// tokens, 5 rows of 32 heads for 8, 84 MB, take 35.5 us, of which the words' decoding, done twice, is half.  (Two blocks of rows under one decoding,
+// One row for a head of the cache is bound by memory: 16 x 4096 tokens of 32 heads of 128, 336 MB, take 62 to 66 us, 5.1 to 5.4 TB/s; the same with all tiles in the L2 caches
+// 49 us, as the vector instructions (88 of them turn a tile's 1024 words of keys into numbers, 88 the values; a softmax of 16 x 32 scores 60; 16 products) are issued in
+// half of the cycles.  Several rows for a head hide nothing more: up to 16 cost what one costs, and every further 16 the reading and the instructions anew: 8 ragged sequences of up to
+// 16003 tokens, 5 rows of 32 heads for 8, take 35.5 us.  Their 80 MB are read twice, 31 us at the rate of a copy, and decoded twice, 43 % of the cycles.  (Two blocks of rows under one decoding,
 // with queries in LDS: 38 us here, 29.5 instead of 35.9 for 32 sequences of 2000 tokens and 3 rows, but 23.7 instead of 14.8 for 1 head for 32 over 32768 tokens, where the
 // joins' work doubles.  Workgroups of both blocks beside each other on one XCD: 36.7.)
-// A single short sequence is a chain of waits: 143 tokens of 32 heads 6.4 us.  512 workgroups are what fits at once: with 1024, half of them ran after the others
+// A single short sequence is a chain of waits: 143 tokens of 32 heads 6.4 us (a workgroup has a head's five tiles, a wavefront one or two of them; nothing is joined).  512 workgroups are what fits at once: with 1024, half of them ran after the others
 // (121 us instead of 75); with 3 or 4 wavefronts a SIMD, the state goes to memory.
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)

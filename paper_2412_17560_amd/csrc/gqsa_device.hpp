@@ -18,7 +18,7 @@ constexpr float kMinusInf = -__builtin_inff();
 // Softmax weights are rounded to fp16, as the second product takes them.  The reference that a row's scores are taken off is held kRoom powers of two below the largest
 // score that it has followed, so that this one has the weight 2^kRoom, and it follows when a score would pass 2^(kRoom + kSlack), which is inside fp16.  What is left below
 // is then fp16's range to 2^-14 and, with fewer bits, 2^-24: a weight vanishes at 2^-32 of the row's largest or below.  (With the largest at 1, at 2^-25: 131072 tokens
-// 17.8 below a first token's score lost four fifths of their sum.)
+// of e^-17.8 times the first one's weight lost four fifths of their sum.)
 constexpr float kSlack = 8.0f, kRoom = 7.0f;
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }

@@ -6,11 +6,14 @@
 // S^T = K Q^T, O^T = V^T P^T -- because then a lane holds scores of one query row only (its maximum and sum need one exchange, between the two
 // halves of the wavefront) and holds them as the second product wants its operand; V^T comes out of LDS by transposing reads.
 //
-// Long prompts are bound by what the matrix cores and the vector units do in turn: 8192 tokens of 32 heads of 128 for 8 (550 GFLOP) take 558 to 595 us, by the card's
-// clock, 985 to 925 TFLOP/s, where a large library product of fp16 reaches 1113.  Without its copies into LDS the kernel takes 502 us, copies alone 217.  Each
-// exponential costs as much as two other instructions, and a tile has 64 of them for every 64 lanes' row; with the weights' sum by dot products of what the second
-// product takes, and the reference that follows only now and then, little else is left beside it.  Ragged batches pay for the diagonal's tiles: 7 sequences of up to 2500
-// tokens, 40 heads for 8, 288 to 308 us, 735 to 785 TFLOP/s of the scores that the mask leaves.  One short prompt is a chain of waits: 15 tokens of 32 heads 5.3 us.
+// Long prompts are bound by what the matrix cores and the vector units do in turn: 8192 tokens of 32 heads of 128 for 8 (550 GFLOP) take 541 to 566 us, by the card's
+// clock, 1016 to 971 TFLOP/s, where a large library product of fp16 reaches 1113; the matrix cores are busy for 53 % of the cycles and the vector units for 46 %.  Without
+// its copies into LDS the kernel takes 503 of 547 us, copies alone 200.  Each exponential costs as much as two other instructions, and a tile has 64 of them for
+// every 64 lanes' row; with the weights' sum by dot products of what the second product takes, and the reference that follows only now and then, little else is
+// left beside it.  Ragged batches pay for blocks that are not full -- the last of a sequence goes through all its keys, with one wavefront of four at work where it
+// has a few rows -- and for the end, when few blocks are left: 7 sequences of up to 2500 tokens, 40 heads for 8, take 290 to 299 us, 781 to 757 TFLOP/s of the scores that the mask
+// leaves.  Counted in tiles a workgroup's share is 16 % more than those scores, the longest row of blocks on one of 512 places 19 %; both units are busy for 76 % of the cycles.
+// One short prompt is a chain of waits: 15 tokens of 32 heads 5.5 us.  In between, one block's keys in turn set the time: 1000 tokens of 40 heads 27 us, 280 TFLOP/s of 1113.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -297,7 +300,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
         for (int i = 0; i < 2 * kPieces; ++i)
 #pragma unroll
             for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2(half2_t{p[i][e], p[i][e + 1]}, ones, sum, false);
-        __builtin_amdgcn_s_setprio(1);      // (products ahead of the other wavefronts' softmax: 2 %)
+        __builtin_amdgcn_s_setprio(1);      // (products ahead of the other wavefronts' softmax: 1.5 % at 8192 tokens)
         // The operand V^T: 16 lanes read 4 keys x 16 elements, each 4 elements of a key, and get 4 keys of an element each.
         const auto turned = [&](const uint16_t* tile, int i, int d) {
             short4_t part[2];
@@ -338,7 +341,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
 #pragma unroll
             for (int r = 0; r < 16; ++r) out[d][r] = f * out[d][r] + g * meet[(2 + 16 * d + r) * 64];
     }
-    // (from the lane's number anew: kept from the loop's start, it would take registers from the loop, 2 %)
+    // (from the lane's number anew: kept from the loop's start, it would take registers from the loop, 1 to 3 %)
     int own_lane = lane;
     asm volatile("" : "+v"(own_lane));
     const int own_row = wave_row0 + (own_lane & 31);
@@ -375,10 +378,10 @@ gqsa_status_t prompt_attend(const PromptCall& call, void* stream)
     c.scale = std::max(std::fabs(c.scale) * 1.44269504088896341f, 1e-30f);
     // Few workgroups: rows shared by two wavefronts, so that there are twice as many.  us of own / shared rows, heads of 128, by the workgroups of 128 rows
     // (bound below):
-    //   keys of 1000 and more: 32: 1 row, 2000 keys, 32 heads 43.7 / 32.5; 224: 2000 x 14 heads 49.9 / 38.1; 256: 2000 rows, 4000 keys, 16 heads 96 / 81; 320: 1000 x 40
-    //     30.4 / 25.5; 352: 1300 x 32 36.3 / 30.9; 384: 1500 x 32 41.5 / 35.3; 448: 4000 x 14 97.6 / 84.2; 576: 1024 x 64 34.2 / 35.7; 2080: 8192 x 32 565 / 671;
-    //   fewer: 64: 128 x 32 8.2 / 7.7; 96: 256 x 32 11.0 / 9.7; 192: 700 x 32 19.8 / 18.1; 256: 900 x 32 25.0 / 22.4; 320: 4 x 194 x 32 12.5 / 12.2; 384: 700 x 64 24.0 / 23.6;
-    //     392: 2 x 800 x 28 27.5 / 27.3; 448: 8 x 100 x 32 8.6 / 9.5; one tile of keys (15 x 32) 5.4 / 5.8, 16 x 64 x 14 6.6 / 7.5.
+    //   keys of 1000 and more: 32: 1 row, 2000 keys, 32 heads 44.5 / 32.4; 224: 2000 x 14 heads 53.3 / 40.1; 256: 2000 rows, 4000 keys, 16 heads 98.6 / 80.1; 320: 1000 x 40
+    //     30.2 / 27.0; 352: 1300 x 32 34.9 / 29.8; 384: 1500 x 32 42.1 / 37.4; 448: 4000 x 14 97.0 / 85.0; 576: 1024 x 64 32.8 / 35.7; 2080: 8192 x 32 for 8 547 / 653;
+    //   fewer: 64: 128 x 32 8.3 / 8.0; 96: 256 x 32 10.9 / 9.6; 192: 700 x 32 19.6 / 17.4; 256: 900 x 32 24.0 / 20.8; 320: 4 x 194 x 32 10.6 / 11.8; 384: 700 x 64 23.2 / 23.9;
+    //     392: 2 x 800 x 28 28.8 / 27.8; 448: 8 x 100 x 32 8.8 / 9.8; one tile of keys (15 x 32) 5.5 / 6.1, 16 x 64 x 14 6.8 / 7.7.
     // (Four tiles in LDS instead of two, where every workgroup has a compute unit for itself, took 1.1 to 1.25 times as long.)
     const auto blocks_of = [&](int rows) { return (c.n_q_rows / rows + c.n_seqs) * c.q_heads; };      // no fewer than there are
     const int64_t whole = blocks_of(kWaves * kWaveRows), half = blocks_of(kWaves * kWaveRows / 2);
@@ -386,9 +389,9 @@ gqsa_status_t prompt_attend(const PromptCall& call, void* stream)
     const int64_t blocks = split ? half : whole;
     if (blocks > (int64_t{1} << 23)) return GQSA_ERR_SHAPE;
     // Blocks of all sequences in the order of their keys, not one sequence after the other, where more of them than run at once would otherwise end with a
-    // long one -- us of either order, ragged lengths up to: 6 x 900, 32 heads 50 / 44.7; 12 x 800 53.1 / 48.7; 30 x 500 53.6 / 50.5; 3 x 1500 62.8 / 60; 20 x 1000, 14 heads of 64
-    // 47.7 / 39 -- but not where the keys and values that an XCD's workgroups are at would then pass its L2 (4 MiB): 7 x 2500, 40 heads 295 / 301; 12 x 3000 554 / 571;
-    // and not where a sequence is a block or so: 64 x 40 21.8 / 22.4.
+    // long one -- us of either order, ragged lengths up to: 6 x 900, 32 heads for 8 63.2 / 60.9; 12 x 800 68.3 / 68.4; 30 x 500 72.2 / 72.5; 3 x 1500 51.6 / 49.9; 20 x 1000, 14 heads
+    // of 64 36.2 / 30.9 -- but not where the keys and values that an XCD's workgroups are at would then pass its L2 (4 MiB): 7 x 2500, 40 heads 294 / 299 or, of other lengths,
+    // 233 / 230; 12 x 3000 391 / 389; nor where a sequence is a block or so, as 64 x 40: 22.8 / 21.9.
     const int64_t heads_at_once = (c.kv_heads + 7) / 8;
     const bool mixed = !split && c.n_seqs > 1 && c.n_seqs <= 64 && blocks > 512 && c.n_k_rows >= int64_t{kWaves} * kWaveRows * c.n_seqs &&
                        c.n_k_rows * c.head_dim * 4 * heads_at_once <= (int64_t{4} << 20);
