@@ -8,12 +8,12 @@
 //
 // Long prompts are bound by what the matrix cores and the vector units do in turn: 8192 tokens of 32 heads of 128 for 8 (550 GFLOP) take 541 to 566 us, by the card's
 // clock, 1016 to 971 TFLOP/s, where a large library product of fp16 reaches 1113; the matrix cores are busy for 53 % of the cycles and the vector units for 46 %.  Without
-// its copies into LDS the kernel takes 503 of 547 us, copies alone 200.  Each exponential costs as much as two other instructions, and a tile has 64 of them for
+// its copies into LDS the kernel takes 502 of 546 us, copies alone 196.  Each exponential costs as much as two other instructions, and a tile has 64 of them for
 // every 64 lanes' row; with the weights' sum by dot products of what the second product takes, and the reference that follows only now and then, little else is
 // left beside it.  Ragged batches pay for blocks that are not full -- the last of a sequence goes through all its keys, with one wavefront of four at work where it
 // has a few rows -- and for the end, when few blocks are left: 7 sequences of up to 2500 tokens, 40 heads for 8, take 290 to 299 us, 781 to 757 TFLOP/s of the scores that the mask
-// leaves.  Counted in tiles a workgroup's share is 16 % more than those scores, the longest row of blocks on one of 512 places 19 %; both units are busy for 76 % of the cycles.
-// One short prompt is a chain of waits: 15 tokens of 32 heads 5.5 us.  In between, one block's keys in turn set the time: 1000 tokens of 40 heads 27 us, 280 TFLOP/s of 1113.
+// leaves.  Counted in tiles a workgroup's share is 16 % more than those scores, the longest row of blocks on one of 512 places 19 %; both units together are busy for 78 % of the cycles.
+// One short prompt is a chain of waits: 15 tokens of 32 heads 5.3 us.  In between, one block's keys in turn set the time: 1000 tokens of 40 heads 27 us, 385 TFLOP/s of 1113.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -94,17 +94,16 @@ __device__ __forceinline__ half8_t finite_part(half8_t v)
 }
 
 // Infinite values.  A row's element is infinite if the row sees one there, and NaN if it sees a NaN or both infinities, whatever the weights; but the product makes NaN of an infinity
-// whose weight is rounded to 0, and so does a rescaling by 0 later on.  So the elements that come out of the loop not finite are put together anew, by the sum of
-// the values that are not finite and that the row sees.  (Called by whole wavefronts, seldom: the wavefront goes once more through its rows' values, 64 keys at a
-// time, and looks closer at keys that hold such a value.)
+// whose weight is rounded to 0, and so does a rescaling by 0 later on.  So elements that see values which are not finite are written anew, as the sum of those
+// values; `to` is where the lane's first element went, null if its row is to stay as it is.  (Called by whole wavefronts, seldom: the wavefront goes once more through
+// its rows' values, 64 keys at a time, and looks closer at keys that hold such a value.)
 template <int D>
-__device__ __forceinline__ void sum_not_finite(const uint16_t* v, int64_t v_row, int keys, int sees, int lane, float16_t (&out)[D / 32])
+__device__ __forceinline__ void write_not_finite(const uint16_t* v, int64_t v_row, int keys, int sees, int lane, uint16_t* to)
 {
     constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes;        // lanes to a key, keys to a load of 16 bytes a lane
+    float16_t sum[D / 32];
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) out[d][r] = __builtin_fabsf(out[d][r]) < __builtin_inff() ? out[d][r] : 0.0f;
+    for (int d = 0; d < D / 32; ++d) sum[d] = float16_t{};
     for (int first = 0; first < keys; first += 64) {
         uint32_t odd = 0;           // bit i: this lane's part of key first + i kAtOnce + lane / kLanes
         u32x4_t x[64 / kAtOnce];
@@ -127,11 +126,17 @@ __device__ __forceinline__ void sum_not_finite(const uint16_t* v, int64_t v_row,
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float value = static_cast<float>(y[e]);
-                        if (key < sees && !(__builtin_fabsf(value) < __builtin_inff())) out[d][4 * r + e] += value;
+                        if (key < sees && !(__builtin_fabsf(value) < __builtin_inff())) sum[d][4 * r + e] += value;
                     }
                 }
         }
     }
+    if (!to) return;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (!(sum[d][r] == 0.0f)) to[32 * d + 8 * (r >> 2) + (r & 3)] = __builtin_bit_cast(uint16_t, static_cast<_Float16>(sum[d][r]));
 }
 
 // The slot-th of the blocks of up to 64 sequences in the order of the keys they see, the most first: `level` is how many times ROWS those are, the last block of
@@ -300,7 +305,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
         for (int i = 0; i < 2 * kPieces; ++i)
 #pragma unroll
             for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2(half2_t{p[i][e], p[i][e + 1]}, ones, sum, false);
-        __builtin_amdgcn_s_setprio(1);      // (products ahead of the other wavefronts' softmax: 1.5 % at 8192 tokens)
+        __builtin_amdgcn_s_setprio(1);      // (products ahead of the other wavefronts' softmax: 1.5 % at 8192 tokens, -3 to 1 % at fewer)
         // The operand V^T: 16 lanes read 4 keys x 16 elements, each 4 elements of a key, and get 4 keys of an element each.
         const auto turned = [&](const uint16_t* tile, int i, int d) {
             short4_t part[2];
@@ -341,31 +346,34 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptCall c, bool 
 #pragma unroll
             for (int r = 0; r < 16; ++r) out[d][r] = f * out[d][r] + g * meet[(2 + 16 * d + r) * 64];
     }
-    // (from the lane's number anew: kept from the loop's start, it would take registers from the loop, 1 to 3 %)
+    // (from the lane's number anew: kept from the loop's start, it would take registers from the loop, up to 5 %)
     int own_lane = lane;
     asm volatile("" : "+v"(own_lane));
     const int own_row = wave_row0 + (own_lane & 31);
-    // (a row whose sum is not finite is NaN throughout)
     float largest_out = 0.0f;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) largest_out = __builtin_elementwise_maximum(largest_out, __builtin_fabsf(out[d][r]));
-    if (__builtin_expect(wild || __any(!(largest_out < __builtin_inff()) && sum < __builtin_inff()), 0))
-        sum_not_finite<D>(reinterpret_cast<const uint16_t*>(v_from), c.v.row, wave_keys, own_row + behind + 1, own_lane, out);
-    if (own_row >= n_q) return;
     // (a row without keys: all sums are 0; one with scores of -infinity only is NaN)
     const float inverse = own_row + behind < 0 ? 0.0f : sum == 0.0f ? __builtin_nanf("") : 1.0f / sum;
     uint16_t* to = c.out.data + (int64_t{q_start} + own_row) * c.out.row + head * c.out.head + 4 * (own_lane >> 5);
+    if (own_row < n_q) {
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
+        for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            half4_t y;
+            for (int r = 0; r < 4; ++r) {
+                half4_t y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = static_cast<_Float16>(out[d][4 * r + e] * inverse);
-            *reinterpret_cast<half4_t*>(to + 32 * d + 8 * r) = y;
-        }
+                for (int e = 0; e < 4; ++e) y[e] = static_cast<_Float16>(out[d][4 * r + e] * inverse);
+                *reinterpret_cast<half4_t*>(to + 32 * d + 8 * r) = y;
+            }
+    }
+    // The second look stands behind the stores: ahead of them, its instructions would have to be jumped over (128 tokens of 32 heads 8.0 us instead of 7.7).  A row whose sum is
+    // not finite, or that has scores of -infinity only, is NaN throughout and stays so.
+    const bool sound = sum > 0.0f && sum < __builtin_inff();
+    if (__builtin_expect(wild || __any(!(largest_out < __builtin_inff()) && sound), 0))
+        write_not_finite<D>(reinterpret_cast<const uint16_t*>(v_from), c.v.row, wave_keys, own_row + behind + 1, own_lane, own_row < n_q && sound ? to : nullptr);
 }
 
 }  // namespace
@@ -378,10 +386,10 @@ gqsa_status_t prompt_attend(const PromptCall& call, void* stream)
     c.scale = std::max(std::fabs(c.scale) * 1.44269504088896341f, 1e-30f);
     // Few workgroups: rows shared by two wavefronts, so that there are twice as many.  us of own / shared rows, heads of 128, by the workgroups of 128 rows
     // (bound below):
-    //   keys of 1000 and more: 32: 1 row, 2000 keys, 32 heads 44.5 / 32.4; 224: 2000 x 14 heads 53.3 / 40.1; 256: 2000 rows, 4000 keys, 16 heads 98.6 / 80.1; 320: 1000 x 40
-    //     30.2 / 27.0; 352: 1300 x 32 34.9 / 29.8; 384: 1500 x 32 42.1 / 37.4; 448: 4000 x 14 97.0 / 85.0; 576: 1024 x 64 32.8 / 35.7; 2080: 8192 x 32 for 8 547 / 653;
-    //   fewer: 64: 128 x 32 8.3 / 8.0; 96: 256 x 32 10.9 / 9.6; 192: 700 x 32 19.6 / 17.4; 256: 900 x 32 24.0 / 20.8; 320: 4 x 194 x 32 10.6 / 11.8; 384: 700 x 64 23.2 / 23.9;
-    //     392: 2 x 800 x 28 28.8 / 27.8; 448: 8 x 100 x 32 8.8 / 9.8; one tile of keys (15 x 32) 5.5 / 6.1, 16 x 64 x 14 6.8 / 7.7.
+    //   keys of 1000 and more: 32: 1 row, 2000 keys, 32 heads 44.1 / 32.2; 224: 2000 x 14 heads 52.9 / 40.0; 256: 2000 rows, 4000 keys, 16 heads 97.7 / 82.0; 320: 1000 x 40
+    //     29.7 / 26.7; 352: 1300 x 32 34.5 / 29.0; 384: 1500 x 32 42.0 / 36.4; 448: 4000 x 14 96.9 / 85.3; 576: 1024 x 64 32.4 / 34.5; 2080: 8192 x 32 for 8 543 / 652;
+    //   fewer: 64: 128 x 32 8.0 / 7.6; 96: 256 x 32 10.5 / 9.3; 192: 700 x 32 19.3 / 17.5; 256: 900 x 32 23.6 / 20.5; 320: 4 x 194 x 32 10.3 / 11.6; 384: 700 x 64 23.0 / 23.0;
+    //     392: 2 x 800 x 28 28.1 / 27.0; 448: 8 x 100 x 32 8.4 / 9.6; one tile of keys (15 x 32) 5.2 / 5.8, 16 x 64 x 14 6.5 / 7.5.
     // (Four tiles in LDS instead of two, where every workgroup has a compute unit for itself, took 1.1 to 1.25 times as long.)
     const auto blocks_of = [&](int rows) { return (c.n_q_rows / rows + c.n_seqs) * c.q_heads; };      // no fewer than there are
     const int64_t whole = blocks_of(kWaves * kWaveRows), half = blocks_of(kWaves * kWaveRows / 2);
@@ -389,9 +397,9 @@ gqsa_status_t prompt_attend(const PromptCall& call, void* stream)
     const int64_t blocks = split ? half : whole;
     if (blocks > (int64_t{1} << 23)) return GQSA_ERR_SHAPE;
     // Blocks of all sequences in the order of their keys, not one sequence after the other, where more of them than run at once would otherwise end with a
-    // long one -- us of either order, ragged lengths up to: 6 x 900, 32 heads for 8 63.2 / 60.9; 12 x 800 68.3 / 68.4; 30 x 500 72.2 / 72.5; 3 x 1500 51.6 / 49.9; 20 x 1000, 14 heads
-    // of 64 36.2 / 30.9 -- but not where the keys and values that an XCD's workgroups are at would then pass its L2 (4 MiB): 7 x 2500, 40 heads 294 / 299 or, of other lengths,
-    // 233 / 230; 12 x 3000 391 / 389; nor where a sequence is a block or so, as 64 x 40: 22.8 / 21.9.
+    // long one -- us of either order, ragged lengths up to: 6 x 900, 32 heads for 8 63.4 / 61.2; 12 x 800 68.3 / 68.4; 30 x 500 72.8 / 72.0; 3 x 1500 52.2 / 50.2; 20 x 1000, 14 heads
+    // of 64 36.7 / 31.0 -- but not where the keys and values that an XCD's workgroups are at would then pass its L2 (4 MiB): 7 x 2500, 40 heads 294 / 300 or, of other lengths,
+    // 235 / 231; 12 x 3000 397 / 394; nor where a sequence is a block or so, as 64 x 40: 21.6 / 21.2.
     const int64_t heads_at_once = (c.kv_heads + 7) / 8;
     const bool mixed = !split && c.n_seqs > 1 && c.n_seqs <= 64 && blocks > 512 && c.n_k_rows >= int64_t{kWaves} * kWaveRows * c.n_seqs &&
                        c.n_k_rows * c.head_dim * 4 * heads_at_once <= (int64_t{4} << 20);
