@@ -1,7 +1,7 @@
 /*
  * gqsa_attention.h -- what lies between the q/k/v products and the o product of a decoder layer: norms of the queries and
  * keys of each head with the rotation by position, a paged cache of keys and values in 4 bits, attention of the newest tokens
- * over that cache (token generation), and causal attention over packed prompts.
+ * over that cache (token generation, one token or a tree of drafted ones at a time), and causal attention over packed prompts.
  *
  * Same conventions as gqsa.h: plain pointers and sizes, [host] or [device], a gqsa_status_t from every call, nothing thrown.
  * Calls only enqueue on `hip_stream` unless said otherwise: a stream of the current HIP device, where all [device] arrays lie.  All
@@ -97,6 +97,26 @@ gqsa_status_t gqsa_cache_append(gqsa_cache_t c, const void* k, int64_t k_row_str
                                 int n_seqs, void* hip_stream);
 
 /*
+ * gqsa_qk_norm_rotate and gqsa_cache_append in one launch: new queries and keys normed and rotated, keys and values quantised into the cache.
+ * The norms' factor 1 / sqrt(mean(x^2) + eps) is computed in 64 bits and rounded to fp32, every other operation is a single fp32 operation: what the cache
+ * holds does not hang on the order of a sum.  (gqsa_qk_norm_rotate adds in fp32: with norms a few elements in 10^4 differ from its by one rounding; without, none does.)
+ *   q        [device] fp16 [n_rows, q_heads, head_dim of the cache]; q_heads 0 .. 1024 (0: q, q_out unused)
+ *   k, v, lengths, pages and the rest as in gqsa_cache_append; q_weight .. interleaved as in gqsa_qk_norm_rotate
+ *   positions  [device] int32 [n_rows], or NULL: a token's place in its sequence
+ *   q_out    like q, k_out like k, or NULL: the rotated keys are wanted in the cache only.  The same arrays as q and k (in place, same distances) or ones that
+ *            overlap nothing else.  Rows that are left out of the cache are normed and rotated all the same; rows that belong to no sequence are left as they are
+ */
+gqsa_status_t gqsa_cache_append_rotated(gqsa_cache_t c, const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads,
+                                        const void* k, int64_t k_row_stride, int64_t k_head_stride,
+                                        const void* v, int64_t v_row_stride, int64_t v_head_stride, int64_t n_rows,
+                                        const void* q_weight, const void* k_weight, float eps,
+                                        const float* table, int64_t n_positions, int rotary_dim, int interleaved, const int32_t* positions,
+                                        void* q_out, int64_t q_out_row_stride, int64_t q_out_head_stride,
+                                        void* k_out, int64_t k_out_row_stride, int64_t k_out_head_stride,
+                                        const int32_t* pages, int max_pages, const int32_t* lengths, const int32_t* row_starts,
+                                        int n_seqs, void* hip_stream);
+
+/*
  * The values that the last tokens of each sequence stand for: row i of the n rows of sequence b is its token lengths[b] - n + i (a whole
  * sequence: n = lengths[b]).  Rows without a token (below 0, beyond the pages, or on an absent page) are zero.
  *   k_out, v_out [device] fp16 [n_rows, kv_heads, head_dim]
@@ -122,6 +142,29 @@ gqsa_status_t gqsa_cache_attend(gqsa_cache_t c, const void* q, int64_t q_row_str
                                 int64_t n_rows, const int32_t* pages, int max_pages, const int32_t* lengths,
                                 const int32_t* row_starts, int n_seqs, float scale, void* out, int64_t out_row_stride,
                                 int64_t out_head_stride, void* hip_stream);
+
+/*
+ * The same for rows that are a tree of drafted tokens (or any others that do not see all rows before their own): row i of the n rows of sequence b sees the
+ * tokens 0 .. lengths[b] - n - 1, which lie before all rows, and of the rows those that its mask names -- itself only if it names it.  A row that
+ * sees no token is zero.
+ *   masks    [device] int32 [n_rows, mask_words]: bit j % 32 of word j / 32 stands for row j of the row's own sequence (bits of rows that it does not have, and rows
+ *            from 32 mask_words on: not seen); mask_words 1 .. 2^15 (GQSA_ERR_UNSUPPORTED)
+ * Keys and values that a row does not see have no effect on it, whatever they hold.  The rest as in gqsa_cache_attend.
+ */
+gqsa_status_t gqsa_cache_attend_tree(gqsa_cache_t c, const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads,
+                                     int64_t n_rows, const int32_t* pages, int max_pages, const int32_t* lengths,
+                                     const int32_t* row_starts, int n_seqs, const int32_t* masks, int mask_words, float scale,
+                                     void* out, int64_t out_row_stride, int64_t out_head_stride, void* hip_stream);
+
+/*
+ * Of the newest rows of each sequence some become neighbours: with n rows of sequence b, whose tokens are lengths[b] - n .. lengths[b] - 1, token lengths[b] - n + i
+ * becomes what token lengths[b] - n + path[row_starts[b] + i] was, for i = 0 .. accepted[b] (path and accepted as gqsa_verify gives them; afterwards the
+ * sequence is lengths[b] - n + accepted[b] + 1 tokens long, which the caller notes).  The tokens behind stay.  Codes are moved as they are: nothing is rounded anew.
+ *   path     [device] int32 [n_rows], accepted [device] int32 [n_seqs] (counts as at most n - 1).  Entries of path that are below i, or n and more, are left out: their token stays
+ *            as it is; so does one whose old or new place lies on an absent page, beyond the pages or below 0
+ */
+gqsa_status_t gqsa_cache_keep(gqsa_cache_t c, int64_t n_rows, const int32_t* pages, int max_pages, const int32_t* lengths, const int32_t* row_starts,
+                              int n_seqs, const int32_t* path, const int32_t* accepted, void* hip_stream);
 
 /*
  * Causal attention over packed prompts: sequence b has the query rows q_starts[b] .. q_starts[b + 1] - 1 and the keys and values

@@ -125,6 +125,18 @@ def _lib():
     lib.gqsa_cache_attend.argtypes = [vp, *heads, i32, i64, *sequences, C.c_float, *heads, vp]
     lib.gqsa_prompt_attend.restype = C.c_int
     lib.gqsa_prompt_attend.argtypes = [*heads, i32, i64, *heads, *heads, i32, i64, i32, vp, vp, i32, C.c_float, *heads, vp]
+    lib.gqsa_cache_append_rotated.restype = C.c_int
+    lib.gqsa_cache_append_rotated.argtypes = [vp, *heads, i32, *heads, *heads, i64, vp, vp, C.c_float, vp, i64, i32, i32, vp, *heads, *heads, *sequences, vp]
+    lib.gqsa_cache_attend_tree.restype = C.c_int
+    lib.gqsa_cache_attend_tree.argtypes = [vp, *heads, i32, i64, *sequences, vp, i32, C.c_float, *heads, vp]
+    lib.gqsa_cache_keep.restype = C.c_int
+    lib.gqsa_cache_keep.argtypes = [vp, i64, *sequences, vp, vp, vp]
+    lib.gqsa_verify_create.restype = C.c_int
+    lib.gqsa_verify_create.argtypes = [i32, i32, C.POINTER(vp)]
+    lib.gqsa_verify_free.restype = None
+    lib.gqsa_verify_free.argtypes = [vp]
+    lib.gqsa_verify.restype = C.c_int
+    lib.gqsa_verify.argtypes = [vp, vp, i64, vp, i64, i32, i64, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
     lib.gqsa_stream_read_workgroups.restype = C.c_int
     lib.gqsa_stream_read_workgroups.argtypes = []
     _LIB = lib
@@ -538,6 +550,22 @@ def _like(x, stream):
         return torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
+def _rotation(table, positions, rows: int, device: int, needs_positions: bool):
+    """(table's pointer, its positions, rotary_dim, pointer of positions) of a rotation, or of none."""
+    if table is None:
+        return None, 0, 0, None
+    at, shape = _flat(table, _FLOAT, "table", device)
+    n_positions, half, two = shape if len(shape) == 3 else (0, 0, 0)
+    if two != 2 or (positions is None and needs_positions):
+        raise ValueError("table must be [n_positions, rotary_dim / 2, 2] and positions [rows]")
+    positions_at = None
+    if positions is not None:
+        positions_at, shape = _flat(positions, _INT, "positions", device)
+        if len(shape) != 1 or shape[0] != rows:
+            raise ValueError("positions must be [rows]")
+    return at, n_positions, 2 * half, positions_at
+
+
 def _norm_weight(w, dim: int, device: int):
     at, shape = _flat(w, _HALF, "norm weights", device)
     if len(shape) != 1 or shape[0] != dim:
@@ -563,17 +591,7 @@ def gqsa_qk_norm_rotate(q, k, positions, table, q_weight=None, k_weight=None, ep
         if k_rows != rows or k_dim != dim:
             raise ValueError("k must be [rows, k_heads, head_dim]")
         ko_at, ko_row, ko_head = _heads_like(k_out, "k_out", rows, k_heads, dim, device)
-    n_positions = rotary = 0
-    table_at = positions_at = None
-    if table is not None:
-        table_at, shape = _flat(table, _FLOAT, "table", device)
-        n_positions, half, two = shape if len(shape) == 3 else (0, 0, 0)
-        if two != 2 or positions is None:
-            raise ValueError("table must be [n_positions, rotary_dim / 2, 2] and positions [rows]")
-        positions_at, shape = _flat(positions, _INT, "positions", device)
-        if len(shape) != 1 or shape[0] != rows:
-            raise ValueError("positions must be [rows]")
-        rotary = 2 * half
+    table_at, n_positions, rotary, positions_at = _rotation(table, positions, rows, device, True)
     q_weight_at = None if q_weight is None else _norm_weight(q_weight, dim, device)
     k_weight_at = None if k_weight is None else _norm_weight(k_weight, dim, device)
     _check(_lib().gqsa_qk_norm_rotate(
@@ -646,6 +664,45 @@ def gqsa_cache_append(c: GqsaCache, k, v, pages, lengths, row_starts=None, strea
                                     _stream_ptr(stream, device)), "gqsa_cache_append")
 
 
+def gqsa_cache_append_rotated(c: GqsaCache, q, k, v, positions, table, pages, lengths, row_starts=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                              interleaved: bool = False, q_out=None, k_out=None, stream=None):
+    """gqsa_qk_norm_rotate of queries [rows, q_heads, head_dim] (or None) and keys and gqsa_cache_append of keys and values in one launch.  positions None: a
+    token's place in its sequence; table None: no rotation; k_out None: the rotated keys go to the cache only.  Returns (q_out, k_out)."""
+    device = _device_of(k)
+    k_at, k_row, k_head, v_at, v_row, v_head, rows = _cache_rows(c, k, v, "k", "v", device)
+    dim = c.head_dim
+    q_at, q_row, q_head, q_heads, qo_at, qo_row, qo_head = None, 0, 0, 0, None, 0, 0
+    if q is not None:
+        q_at, q_row, q_head, q_rows, q_heads, q_dim = _heads(q, "q", device)
+        if q_rows != rows or q_dim != dim:
+            raise ValueError("q must be [rows, q_heads, head_dim] of the cache")
+        if q_out is None:
+            q_out = _like(q, stream)
+        qo_at, qo_row, qo_head = _heads_like(q_out, "q_out", rows, q_heads, dim, device)
+    ko_at, ko_row, ko_head = (None, 0, 0) if k_out is None else _heads_like(k_out, "k_out", rows, c.kv_heads, dim, device)
+    table_at, n_positions, rotary, positions_at = _rotation(table, positions, rows, device, False)
+    q_weight_at = None if q_weight is None else _norm_weight(q_weight, dim, device)
+    k_weight_at = None if k_weight is None else _norm_weight(k_weight, dim, device)
+    _check(_lib().gqsa_cache_append_rotated(
+        c.ptr, q_at, q_row, q_head, q_heads, k_at, k_row, k_head, v_at, v_row, v_head, rows, q_weight_at, k_weight_at, eps, table_at, n_positions, rotary,
+        interleaved, positions_at, qo_at, qo_row, qo_head, ko_at, ko_row, ko_head, *_sequences(pages, lengths, row_starts, device),
+        _stream_ptr(stream, device)), "gqsa_cache_append_rotated")
+    return q_out, k_out
+
+
+def gqsa_cache_keep(c: GqsaCache, pages, lengths, row_starts, path, accepted, stream=None) -> None:
+    """Of the newest rows of each sequence, those of path (int32 [rows], as gqsa_verify gives it) become the first accepted + 1 (accepted int32 [n_seqs])."""
+    device = _device_of(path)
+    if _INT is None:
+        _names()
+    path_at, path_shape = _flat(path, _INT, "path", device)
+    where = _sequences(pages, lengths, row_starts, device)
+    accepted_at, accepted_shape = _flat(accepted, _INT, "accepted", device)
+    if len(path_shape) != 1 or len(accepted_shape) != 1 or accepted_shape[0] != where[4]:
+        raise ValueError("path must be [rows] and accepted [n_seqs]")
+    _check(_lib().gqsa_cache_keep(c.ptr, path_shape[0], *where, path_at, accepted_at, _stream_ptr(stream, device)), "gqsa_cache_keep")
+
+
 def gqsa_cache_read(c: GqsaCache, pages, lengths, row_starts, k_out, v_out, stream=None):
     """The values of the last tokens of each sequence, as many as it has rows in k_out and v_out [rows, kv_heads, head_dim]."""
     device = _device_of(k_out)
@@ -667,6 +724,98 @@ def gqsa_cache_attend(c: GqsaCache, q, pages, lengths, row_starts=None, scale: f
                                     dim ** -0.5 if scale is None else scale, out_at, out_row, out_head, _stream_ptr(stream, device)),
            "gqsa_cache_attend")
     return out
+
+
+def gqsa_cache_attend_tree(c: GqsaCache, q, pages, lengths, row_starts, masks, scale: float = None, out=None, stream=None):
+    """gqsa_cache_attend where a row sees the tokens before all rows of its sequence, and of these rows those that its mask names: masks int32
+    [rows, mask_words], bit j % 32 of word j / 32 for row j of the sequence."""
+    device = _device_of(q)
+    q_at, q_row, q_head, rows, heads, dim = _heads(q, "q", device)
+    if dim != c.head_dim:
+        raise ValueError("q must be [rows, q_heads, head_dim] of the cache")
+    masks_at, shape = _flat(masks, _INT, "masks", device)
+    if len(shape) != 2 or shape[0] != rows:
+        raise ValueError("masks must be [rows, mask_words]")
+    if out is None:
+        out = _like(q, stream)
+    out_at, out_row, out_head = _heads_like(out, "out", rows, heads, dim, device)
+    _check(_lib().gqsa_cache_attend_tree(c.ptr, q_at, q_row, q_head, heads, rows, *_sequences(pages, lengths, row_starts, device), masks_at, shape[1],
+                                         dim ** -0.5 if scale is None else scale, out_at, out_row, out_head, _stream_ptr(stream, device)),
+           "gqsa_cache_attend_tree")
+    return out
+
+
+class GqsaVerifier:
+    """Owns one gqsa_verifier_t; freed on gqsa_verify_free() or garbage collection."""
+
+    def __init__(self, ptr: int):
+        self.ptr = C.c_void_p(ptr)
+
+    def __del__(self):
+        try:
+            gqsa_verify_free(self)
+        except Exception:
+            pass
+
+
+def gqsa_verify_create(max_seqs: int, max_vocab: int) -> GqsaVerifier:
+    out = C.c_void_p()
+    _check(_lib().gqsa_verify_create(max_seqs, max_vocab, C.byref(out)), "gqsa_verify_create")
+    return GqsaVerifier(out.value)
+
+
+def gqsa_verify_free(v: GqsaVerifier) -> None:
+    """The workspace must not be in use any more (as with gqsa_free, calls that use it have to be over)."""
+    if v.ptr is not None and v.ptr.value:
+        _lib().gqsa_verify_free(v.ptr)
+        v.ptr = C.c_void_p()
+
+
+def _probabilities(t, what: str, device: int):
+    """(pointer, distance between rows, rows, vocabulary) of a float32 tensor [rows, vocabulary] on that device with contiguous rows."""
+    try:
+        rows, vocab = t.shape
+        row, one = t.stride()
+        if (one == 1 or vocab == 1 or rows == 0) and t.dtype is _FLOAT and t.get_device() == device:
+            return t.data_ptr(), row if rows > 1 else vocab, rows, vocab
+    except (AttributeError, TypeError, ValueError):
+        pass
+    raise ValueError(f"{what} must be a float32 device tensor [rows, vocabulary] with contiguous rows, on the device of the others")
+
+
+def _numbers(t, dtype, what: str, n: int, device: int):
+    at, shape = _flat(t, dtype, what, device)
+    if len(shape) != 1 or shape[0] != n:
+        raise ValueError(f"{what} must be [{n}]")
+    return at
+
+
+def gqsa_verify(v: GqsaVerifier, target, tokens, uniforms, finals, row_starts=None, parents=None, draft=None, path=None, out=None, accepted=None, stream=None):
+    """Which drafted tokens (int32 [rows], row 0 of a sequence the last certain one) the target's probabilities (float32 [rows, vocabulary]) let stand, and
+    one more token behind them.  parents int32 [rows] (None: chains), draft float32 [rows, vocabulary] what chains were drawn from (or None), uniforms
+    float32 [rows] and finals float32 [n_seqs] from [0, 1).  Returns (path, out, accepted), int32 [rows], [rows], [n_seqs]."""
+    device = _device_of(target)
+    if _INT is None:
+        _names()
+    target_at, target_row, rows, vocab = _probabilities(target, "target", device)
+    draft_at, draft_row = None, 0
+    if draft is not None:
+        draft_at, draft_row, d_rows, d_vocab = _probabilities(draft, "draft", device)
+        if d_rows != rows or d_vocab != vocab:
+            raise ValueError("draft must be like target")
+    tokens_at = _numbers(tokens, _INT, "tokens", rows, device)
+    uniforms_at = _numbers(uniforms, _FLOAT, "uniforms", rows, device)
+    finals_at, shape = _flat(finals, _FLOAT, "finals", device)
+    n_seqs = shape[0] if len(shape) == 1 else -1
+    parents_at = None if parents is None else _numbers(parents, _INT, "parents", rows, device)
+    starts_at = None if row_starts is None else _numbers(row_starts, _INT, "row_starts", n_seqs + 1, device)
+    path = _like(tokens, stream) if path is None else path
+    out = _like(tokens, stream) if out is None else out
+    accepted = _like(finals, stream).view(_INT) if accepted is None else accepted
+    _check(_lib().gqsa_verify(v.ptr, target_at, target_row, draft_at, draft_row, vocab, rows, tokens_at, parents_at, uniforms_at, finals_at, starts_at, n_seqs,
+                              _numbers(path, _INT, "path", rows, device), _numbers(out, _INT, "out", rows, device),
+                              _numbers(accepted, _INT, "accepted", n_seqs, device), _stream_ptr(stream, device)), "gqsa_verify")
+    return path, out, accepted
 
 
 def gqsa_prompt_attend(q, k, v, q_starts, k_starts, scale: float = None, out=None, stream=None):

@@ -1,5 +1,5 @@
 // Internal definitions of the operators between the q/k/v and the o product (include/gqsa_attention.h): what the C boundary
-// (gqsa_attention_api.cpp) hands to the kernels (gqsa_rotate.hip, gqsa_cache.hip, gqsa_prompt.hip).
+// (gqsa_attention_api.cpp) hands to the kernels (gqsa_rotate.hip, gqsa_cache.hip, gqsa_cache_rows.hip, gqsa_prompt.hip).
 #pragma once
 
 #include <cstdint>
@@ -88,6 +88,10 @@ void cache_release(gqsa_cache* c);
 gqsa_status_t cache_append(gqsa_cache* c, const Heads& k, const Heads& v, const Sequences& seqs, void* stream);
 gqsa_status_t cache_read(gqsa_cache* c, const Heads& k, const Heads& v, const Sequences& seqs, void* stream);
 gqsa_status_t cache_attend(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, float scale, const Heads& out, void* stream);
+gqsa_status_t cache_append_rotated(gqsa_cache* c, const RotateCall& call, const Heads& v, const Sequences& seqs, void* stream);
+gqsa_status_t cache_attend_tree(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, const uint32_t* masks, int mask_words, float scale,
+                                const Heads& out, void* stream);
+gqsa_status_t cache_keep(gqsa_cache* c, const Sequences& seqs, const int32_t* path, const int32_t* accepted, void* stream);
 
 struct PromptCall {
     Heads q, k, v, out;

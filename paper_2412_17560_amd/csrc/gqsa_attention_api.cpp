@@ -43,6 +43,28 @@ gqsa_status_t take_sequences(const int32_t* pages, int max_pages, const int32_t*
     return GQSA_OK;
 }
 
+// Norms and rotation of a call; `any_positions`: a NULL is a token's place.
+gqsa_status_t take_rotation(const void* q_weight, const void* k_weight, float eps, const float* table, int64_t n_positions, int rotary_dim, int interleaved,
+                            const int32_t* positions, bool any_positions, int head_dim, gqsa::RotateCall* c)
+{
+    if (n_positions < 0) return GQSA_ERR_SHAPE;
+    if (head_dim < 16 || head_dim > 256 || head_dim % 16 != 0) return GQSA_ERR_UNSUPPORTED;
+    if (rotary_dim < 0 || rotary_dim > head_dim || rotary_dim % 16 != 0) return GQSA_ERR_UNSUPPORTED;
+    if (rotary_dim > 0 && (!table || (!positions && !any_positions))) return GQSA_ERR_NULL;
+    if (!aligned(q_weight, 16) || !aligned(k_weight, 16) || !aligned(table, 16) || !aligned(positions, 4)) return GQSA_ERR_ALIGN;
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return GQSA_ERR_RANGE;
+    c->q_weight = static_cast<const uint16_t*>(q_weight);
+    c->k_weight = static_cast<const uint16_t*>(k_weight);
+    c->table = table;
+    c->positions = positions;
+    c->n_positions = n_positions;
+    c->head_dim = head_dim;
+    c->rotary_dim = rotary_dim;
+    c->interleaved = interleaved != 0;
+    c->eps = eps;
+    return GQSA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -64,23 +86,10 @@ gqsa_status_t gqsa_qk_norm_rotate(const void* q, int64_t q_row_stride, int64_t q
         if (gqsa_status_t st = take(k, k_row_stride, k_head_stride, &c.k)) return st;
         if (gqsa_status_t st = take(k_out, k_out_row_stride, k_out_head_stride, &c.k_out)) return st;
     }
-    if (head_dim < 16 || head_dim > 256 || head_dim % 16 != 0) return GQSA_ERR_UNSUPPORTED;
-    if (rotary_dim < 0 || rotary_dim > head_dim || rotary_dim % 16 != 0) return GQSA_ERR_UNSUPPORTED;
-    if (rotary_dim > 0 && (!table || !positions)) return GQSA_ERR_NULL;
-    if (!aligned(q_weight, 16) || !aligned(k_weight, 16) || !aligned(table, 16) || !aligned(positions, 4)) return GQSA_ERR_ALIGN;
-    if (!(eps >= 0.0f) || !std::isfinite(eps)) return GQSA_ERR_RANGE;
-    c.q_weight = static_cast<const uint16_t*>(q_weight);
-    c.k_weight = static_cast<const uint16_t*>(k_weight);
-    c.table = table;
-    c.positions = positions;
+    if (gqsa_status_t st = take_rotation(q_weight, k_weight, eps, table, n_positions, rotary_dim, interleaved, positions, false, head_dim, &c)) return st;
     c.n_rows = n_rows;
-    c.n_positions = n_positions;
     c.q_heads = q_heads;
     c.k_heads = k_heads;
-    c.head_dim = head_dim;
-    c.rotary_dim = rotary_dim;
-    c.interleaved = interleaved != 0;
-    c.eps = eps;
     c.one_over_dim = 1.0f / static_cast<float>(head_dim);
     return gqsa::rotate(c, hip_stream);
 }
@@ -143,6 +152,50 @@ gqsa_status_t gqsa_cache_append(gqsa_cache_t c, const void* k, int64_t k_row_str
     return gqsa::cache_append(c, kh, vh, seqs, hip_stream);
 }
 
+gqsa_status_t gqsa_cache_append_rotated(gqsa_cache_t c, const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads,
+                                        const void* k, int64_t k_row_stride, int64_t k_head_stride,
+                                        const void* v, int64_t v_row_stride, int64_t v_head_stride, int64_t n_rows,
+                                        const void* q_weight, const void* k_weight, float eps,
+                                        const float* table, int64_t n_positions, int rotary_dim, int interleaved, const int32_t* positions,
+                                        void* q_out, int64_t q_out_row_stride, int64_t q_out_head_stride,
+                                        void* k_out, int64_t k_out_row_stride, int64_t k_out_head_stride,
+                                        const int32_t* pages, int max_pages, const int32_t* lengths, const int32_t* row_starts,
+                                        int n_seqs, void* hip_stream)
+{
+    if (!c) return GQSA_ERR_NULL;
+    if (n_rows == 0) return GQSA_OK;
+    gqsa::RotateCall call{};
+    gqsa::Heads vh;
+    gqsa::Sequences seqs;
+    if (q_heads < 0) return GQSA_ERR_SHAPE;
+    if (q_heads > kMaxHeads) return GQSA_ERR_UNSUPPORTED;
+    if (q_heads > 0) {
+        if (gqsa_status_t st = take(q, q_row_stride, q_head_stride, &call.q)) return st;
+        if (gqsa_status_t st = take(q_out, q_out_row_stride, q_out_head_stride, &call.q_out)) return st;
+    }
+    if (gqsa_status_t st = take(k, k_row_stride, k_head_stride, &call.k)) return st;
+    if (gqsa_status_t st = take(v, v_row_stride, v_head_stride, &vh)) return st;
+    if (k_out) {
+        if (gqsa_status_t st = take(k_out, k_out_row_stride, k_out_head_stride, &call.k_out)) return st;
+    }
+    if (gqsa_status_t st = take_rotation(q_weight, k_weight, eps, table, n_positions, rotary_dim, interleaved, positions, true, c->head_dim, &call)) return st;
+    if (gqsa_status_t st = take_sequences(pages, max_pages, lengths, row_starts, n_seqs, n_rows, &seqs)) return st;
+    call.q_heads = q_heads;
+    return gqsa::cache_append_rotated(c, call, vh, seqs, hip_stream);
+}
+
+gqsa_status_t gqsa_cache_keep(gqsa_cache_t c, int64_t n_rows, const int32_t* pages, int max_pages, const int32_t* lengths, const int32_t* row_starts,
+                              int n_seqs, const int32_t* path, const int32_t* accepted, void* hip_stream)
+{
+    if (!c) return GQSA_ERR_NULL;
+    if (n_rows == 0) return GQSA_OK;
+    gqsa::Sequences seqs;
+    if (gqsa_status_t st = take_sequences(pages, max_pages, lengths, row_starts, n_seqs, n_rows, &seqs)) return st;
+    if (!path || !accepted) return GQSA_ERR_NULL;
+    if (!aligned(path, 4) || !aligned(accepted, 4)) return GQSA_ERR_ALIGN;
+    return gqsa::cache_keep(c, seqs, path, accepted, hip_stream);
+}
+
 gqsa_status_t gqsa_cache_read(gqsa_cache_t c, void* k_out, int64_t k_row_stride, int64_t k_head_stride,
                               void* v_out, int64_t v_row_stride, int64_t v_head_stride, int64_t n_rows,
                               const int32_t* pages, int max_pages, const int32_t* lengths, const int32_t* row_starts,
@@ -158,6 +211,17 @@ gqsa_status_t gqsa_cache_read(gqsa_cache_t c, void* k_out, int64_t k_row_stride,
     return gqsa::cache_read(c, kh, vh, seqs, hip_stream);
 }
 
+static gqsa_status_t take_attention(gqsa_cache_t c, const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads, int64_t n_rows,
+                                    const int32_t* pages, int max_pages, const int32_t* lengths, const int32_t* row_starts, int n_seqs, float scale,
+                                    void* out, int64_t out_row_stride, int64_t out_head_stride, gqsa::Heads* qh, gqsa::Heads* oh, gqsa::Sequences* seqs)
+{
+    if (gqsa_status_t st = take(q, q_row_stride, q_head_stride, qh)) return st;
+    if (gqsa_status_t st = take(out, out_row_stride, out_head_stride, oh)) return st;
+    if (gqsa_status_t st = check_heads(q_heads, c->kv_heads)) return st;
+    if (gqsa_status_t st = take_sequences(pages, max_pages, lengths, row_starts, n_seqs, n_rows, seqs)) return st;
+    return std::isfinite(scale) ? GQSA_OK : GQSA_ERR_RANGE;
+}
+
 gqsa_status_t gqsa_cache_attend(gqsa_cache_t c, const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads,
                                 int64_t n_rows, const int32_t* pages, int max_pages, const int32_t* lengths,
                                 const int32_t* row_starts, int n_seqs, float scale, void* out, int64_t out_row_stride,
@@ -167,12 +231,29 @@ gqsa_status_t gqsa_cache_attend(gqsa_cache_t c, const void* q, int64_t q_row_str
     if (n_rows == 0) return GQSA_OK;
     gqsa::Heads qh, oh;
     gqsa::Sequences seqs;
-    if (gqsa_status_t st = take(q, q_row_stride, q_head_stride, &qh)) return st;
-    if (gqsa_status_t st = take(out, out_row_stride, out_head_stride, &oh)) return st;
-    if (gqsa_status_t st = check_heads(q_heads, c->kv_heads)) return st;
-    if (gqsa_status_t st = take_sequences(pages, max_pages, lengths, row_starts, n_seqs, n_rows, &seqs)) return st;
-    if (!std::isfinite(scale)) return GQSA_ERR_RANGE;
+    if (gqsa_status_t st = take_attention(c, q, q_row_stride, q_head_stride, q_heads, n_rows, pages, max_pages, lengths, row_starts, n_seqs, scale,
+                                          out, out_row_stride, out_head_stride, &qh, &oh, &seqs))
+        return st;
     return gqsa::cache_attend(c, qh, q_heads, seqs, scale, oh, hip_stream);
+}
+
+gqsa_status_t gqsa_cache_attend_tree(gqsa_cache_t c, const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads,
+                                     int64_t n_rows, const int32_t* pages, int max_pages, const int32_t* lengths,
+                                     const int32_t* row_starts, int n_seqs, const int32_t* masks, int mask_words, float scale,
+                                     void* out, int64_t out_row_stride, int64_t out_head_stride, void* hip_stream)
+{
+    if (!c) return GQSA_ERR_NULL;
+    if (n_rows == 0) return GQSA_OK;
+    gqsa::Heads qh, oh;
+    gqsa::Sequences seqs;
+    if (gqsa_status_t st = take_attention(c, q, q_row_stride, q_head_stride, q_heads, n_rows, pages, max_pages, lengths, row_starts, n_seqs, scale,
+                                          out, out_row_stride, out_head_stride, &qh, &oh, &seqs))
+        return st;
+    if (!masks) return GQSA_ERR_NULL;
+    if (mask_words < 1) return GQSA_ERR_SHAPE;
+    if (mask_words > (1 << 15)) return GQSA_ERR_UNSUPPORTED;
+    if (!aligned(masks, 4)) return GQSA_ERR_ALIGN;
+    return gqsa::cache_attend_tree(c, qh, q_heads, seqs, reinterpret_cast<const uint32_t*>(masks), mask_words, scale, oh, hip_stream);
 }
 
 gqsa_status_t gqsa_prompt_attend(const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads, int64_t n_q_rows,

@@ -1,145 +1,15 @@
 // A paged cache of keys and values in 4 bits (gqsa_cache_append, gqsa_cache_read) and the attention of the newest tokens over it
 // (gqsa_cache_attend).
-//
-// 32 tokens of one head are a tile, laid out as the matrix cores take it, so that a wavefront's loads are whole runs of memory and
-// a lane finds the 8 elements of its operand in one word (D = head_dim, l = lane, quad = l / 16):
-//   keys     D / 16 words a lane; word j D / 32 + g: elements 32 g + 8 quad .. + 7 of token 16 j + l % 16;
-//   values   D / 16 words a lane; word c: element 16 c + l % 16 of the tokens 4 quad .. + 3 and 16 + 4 quad .. + 3;
-//            (words w of all lanes: byte (w / 4) 1024 + l 16 + (w % 4) 4 of the region)
-//   key parameters    token by token, group by group: low, step;
-//   value parameters  group by group, quad by quad: step of those 8 tokens, low of those 8 tokens.
-// Code e of a word is at bits 8 (e % 4) + 4 (e / 4), so that one AND leaves four neighbouring ones in the bytes of a register.
+// (gqsa_cache.hpp says in which order a tile of the cache is held.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <climits>
 #include <cmath>
 
-#include "gqsa_device.hpp"
+#include "gqsa_cache.hpp"
 
 namespace gqsa {
 namespace {
-
-constexpr int kThreads = 256;
-
-__host__ __device__ constexpr int word_offset(int w, int lane) { return (w >> 2) * 1024 + lane * 16 + (w & 3) * 4; }
-__host__ __device__ constexpr int nibble(int e) { return 8 * (e & 3) + 4 * (e >> 2); }
-// The token of slot i of a word of value codes, and back.
-__host__ __device__ constexpr int slot_token(int quad, int i) { return 4 * quad + (i & 3) + (i & 4) * 4; }
-
-struct Pool {
-    uint8_t* base;
-    int64_t n_pages;
-    int page_shift, kv_heads;      // log2 of a page's tokens
-
-    template <int D>
-    __device__ uint8_t* tile(int64_t page, int head, int tile_of_sequence) const
-    {
-        const int tiles = 1 << (page_shift - 5);
-        return base + ((page * kv_heads + head) * tiles + (tile_of_sequence & (tiles - 1))) * int64_t{tile_bytes(D)};
-    }
-};
-
-struct Sequence {
-    int start, rows, length;       // its rows are start .. start + rows - 1, its tokens 0 .. length - 1, the last of them those of the rows
-};
-
-// (a length counts as at least 0 and at most `most`)
-__device__ __forceinline__ Sequence sequence(const Sequences& s, int most, int b)
-{
-    const Rows rows = rows_between(s.row_starts ? s.row_starts[b] : b, s.row_starts ? s.row_starts[b + 1] : b + 1, s.n_rows);
-    Sequence q;
-    q.start = rows.start;
-    q.rows = rows.count;
-    q.length = min(max(s.lengths[b], 0), most);
-    return q;
-}
-
-// What a sequence's pages hold, if they are all there.
-__device__ __forceinline__ int most_tokens(const Sequences& s, int page_shift)
-{
-    return static_cast<int>(min(int64_t{s.max_pages} << page_shift, int64_t{INT_MAX - 4096}));
-}
-
-// --------------------------------------------------------------------------- into the cache and out of it
-struct CopyArgs {
-    Pool pool;
-    Heads k, v;
-    Sequences seqs;
-};
-
-// The tiles that the rows of a sequence lie in, from the first one's (which may be below 0) to the last one's (which may lie beyond the pages).
-__device__ __forceinline__ int tiles_of_rows(const Sequence& q)
-{
-    return q.rows == 0 ? 0 : ((q.length - 1) >> 5) - ((q.length - q.rows) >> 5) + 1;
-}
-
-struct Unit {
-    Sequence seq;
-    int tile, head;
-    int64_t page;       // -1: none
-};
-
-__device__ __forceinline__ bool unit_of(const CopyArgs& a, Unit* u)
-{
-    const auto deal = deal_out<Sequence>(a.seqs.n_seqs, threadIdx.x & 63, [&](int s) { return sequence(a.seqs, INT_MAX, s); },
-                                         [](const Sequence& q) { return static_cast<unsigned>(tiles_of_rows(q)); });
-    if (blockIdx.x >= deal.total) return false;
-    int b, within;
-    u->seq = deal.locate(blockIdx.x, &b, &within);
-    u->tile = ((u->seq.length - u->seq.rows) >> 5) + within;
-    u->head = blockIdx.y;
-    u->page = -1;
-    const int of = u->tile >> (a.pool.page_shift - 5);
-    if (of >= 0 && of < a.seqs.max_pages) {        // (a row beyond the pages is left out, not written over the last token)
-        const int page = a.seqs.pages[int64_t{b} * a.seqs.max_pages + of];
-        if (page >= 0 && page < a.pool.n_pages) u->page = page;
-    }
-    return true;
-}
-
-template <int N>
-struct Quantised {
-    _Float16 low, step;
-    uint32_t code[N];
-};
-
-// N elements of a group whose other elements are with the neighbouring 32 / N - 1 lanes.
-template <int N>
-__device__ __forceinline__ Quantised<N> quantise(const half8_t (&x)[N / 8])
-{
-    float low = __builtin_inff(), high = -__builtin_inff();
-    int bad = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float v = static_cast<float>(x[i / 8][i % 8]);
-        bad |= !(__builtin_fabsf(v) <= 65504.0f);
-        low = fminf(low, v), high = fmaxf(high, v);
-    }
-#pragma unroll
-    for (int d = 1; d < 32 / N; d *= 2) {
-        low = fminf(low, __shfl_xor(low, d)), high = fmaxf(high, __shfl_xor(high, d));
-        bad |= __shfl_xor(bad, d);
-    }
-    Quantised<N> q;
-    q.low = bad ? static_cast<_Float16>(__builtin_nanf("")) : static_cast<_Float16>(low);
-    uint16_t step_bits = __builtin_bit_cast(uint16_t, static_cast<_Float16>(bad ? 0.0f : (high - low) / 15.0f));
-    // (what the largest code would stand for, rounded once as it is when it is read: a sum rounded to fp32 first reaches 65520, from where on fp16 is infinity, too soon)
-    if (__builtin_fmaf16(static_cast<_Float16>(15.0f), __builtin_bit_cast(_Float16, step_bits), q.low) > static_cast<_Float16>(65504.0f)) --step_bits;
-    q.step = __builtin_bit_cast(_Float16, step_bits);
-    // (x - low) / step as one rounded division: with the rounded reciprocal, a product, its exact remainder and one correction.  The corrected
-    // quotient is off by 2^-23 of its last place before it is rounded, and no quotient by a number of 11 bits lies that near to the middle
-    // between two fp32 numbers, so the rounding is the division's.
-    const float step = static_cast<float>(q.step), divisor = step > 0.0f ? step : 1.0f, inverse = 1.0f / divisor;
-    const float highest = step > 0.0f ? 15.0f : 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float over = static_cast<float>(x[i / 8][i % 8]) - low, first = over * inverse;
-        const float quotient = __builtin_fmaf(__builtin_fmaf(-first, divisor, over), inverse, first);
-        q.code[i] = static_cast<uint32_t>(fmaxf(fminf(__builtin_rintf(quotient), highest), 0.0f));
-    }
-    return q;
-}
 
 // One workgroup per tile that gets rows, and head: 8 threads to a token.  The tile is put together in LDS -- a word of key codes is of one token, but one of
 // value codes of 8 -- and written in runs of 16 bytes; of a tile that keeps earlier tokens, only the new ones' words and halves are
@@ -299,6 +169,8 @@ struct AttendArgs {
     int heads_per_group;
     float scale_log2;       // |scale| times log2(e): the softmax is taken to base 2
     bool negate;            // the queries, as scale is negative: the largest score is then the one of the largest product
+    const uint32_t* masks;  // of a tree: which of its sequence's rows a row sees, 32 of them a word
+    int mask_words;
 };
 
 // A tile as it is loaded: codes of keys and of values, parameters (16 bytes a lane with D = 128, 8 with D = 64).
@@ -374,9 +246,10 @@ __device__ __forceinline__ int opaque(int v)
 
 // One tile for one wavefront.  S^T = K Q^T and O^T = V^T P^T: a lane's scores are then the elements of the operand P^T that the second product wants
 // from it, whatever the tokens' order, as the value codes lie in the same.
-template <int D, bool EDGE>
+// With TREE a row sees the tile's tokens that `seen` names, else those below `limit`.
+template <int D, bool EDGE, bool TREE>
 __device__ __forceinline__ void attend_tile(const Raw<D>& raw, uint32_t* stage, const half8_t (&q)[D / 32], RowState<D>& state, int lane,
-                                            int length, int limit, float scale_log2)
+                                            int length, int limit, uint32_t seen, float scale_log2)
 {
     const int first_token = raw.first_token;
     typedef typename Raw<D>::words_t words_t;
@@ -447,7 +320,12 @@ __device__ __forceinline__ void attend_tile(const Raw<D>& raw, uint32_t* stage, 
             value[c] = join(v[0], v[1], v[2], v[3]);
         }
     }
-    if constexpr (EDGE) {
+    if constexpr (EDGE && TREE) {
+        const uint32_t sees = seen >> 4 * opaque(quad);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!(sees >> slot_token(0, i) & 1)) s[i >> 2][i & 3] = kMinusInf;
+    } else if constexpr (EDGE) {
         const int left = limit - first_token - 4 * opaque(quad);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -480,11 +358,21 @@ __device__ __forceinline__ void attend_tile(const Raw<D>& raw, uint32_t* stage, 
     for (int c = 0; c < D / 16; ++c) state.out[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value[c], p, state.out[c], 0, 0, 0);
     if (EDGE && wild) {
         const int left = limit - first_token;
-        const uint32_t sees = left >= 32 ? ~0u : (1u << max(left, 0)) - 1u;
+        const uint32_t sees = TREE ? seen : left >= 32 ? ~0u : (1u << max(left, 0)) - 1u;
 #pragma unroll
         for (int g = 0; g < D / 32; ++g)
             if (nan_of[g] & sees) state.out[2 * g] = state.out[2 * g + 1] = __builtin_nanf("") + float4_t{};
     }
+}
+
+// Of a tree's row, which of the tile's 32 tokens it sees: those before all rows, and those of the rows that its mask names.  `from`: the row whose token is the
+// tile's first (below 0: that many tokens before the rows); `left`: tokens from there to the sequence's end.
+__device__ __forceinline__ uint32_t seen_of(const uint32_t* mask, int words, int from, int left)
+{
+    const int w = from >> 5, shift = from & 31;
+    const auto word = [&](int i) { return i < 0 ? ~0u : i < words ? mask[i] : 0u; };
+    const uint64_t both = uint64_t{word(w + 1)} << 32 | word(w);
+    return static_cast<uint32_t>(both >> shift) & (left >= 32 ? ~0u : (1u << max(left, 0)) - 1u);
 }
 
 __device__ __forceinline__ float weight_of(float top, float most) { return top == kMinusInf ? 0.0f : __builtin_amdgcn_exp2f(top - most); }
@@ -629,7 +517,7 @@ constexpr unsigned kFewSteps = 2;
 // joins' work doubles.  Workgroups of both blocks beside each other on one XCD: 36.7.)
 // A single short sequence is a chain of waits: 143 tokens of 32 heads 6.4 us (a workgroup has a head's five tiles, a wavefront one or two of them; nothing is joined).  512 workgroups are what fits at once: with 1024, half of them ran after the others
 // (121 us instead of 75); with 3 or 4 wavefronts a SIMD, the state goes to memory.
-template <int D, int WAVES>
+template <int D, int WAVES, bool TREE>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
 {
     constexpr int kThreads = 64 * WAVES;
@@ -692,7 +580,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
             if (a.negate) q[g] = -q[g];
             q[g] += q[g] - q[g];
         }
-        const int least = before + token0 + 1, most = before + token0 + (head0 + rows - 1) / per + 1;    // tokens that the block's first and last row see
+        // tokens that the block's first and last row see; of a tree, the tokens before the rows and all
+        const int least = TREE ? before : before + token0 + 1, most = TREE ? seq.length : before + token0 + (head0 + rows - 1) / per + 1;
         const int tiles = uniform(min((max(most, 0) + kTileTokens - 1) / kTileTokens, to * step_tiles));
 
         RowState<D> state;
@@ -724,8 +613,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
         };
         const auto attend = [&](const Raw<D>& raw) {
             if (raw.first_token < 0) return;
-            if (raw.first_token + kTileTokens > least) attend_tile<D, true>(raw, shared.stage[wave], q, state, lane, seq.length, limit, a.scale_log2);
-            else attend_tile<D, false>(raw, shared.stage[wave], q, state, lane, seq.length, limit, a.scale_log2);
+            if (raw.first_token + kTileTokens > least) {
+                uint32_t seen = 0;
+                if constexpr (TREE) {
+                    if (is_row) seen = seen_of(a.masks + int64_t{seq.start + row} * a.mask_words, a.mask_words, raw.first_token - before, seq.length - raw.first_token);
+                }
+                attend_tile<D, true, TREE>(raw, shared.stage[wave], q, state, lane, seq.length, limit, seen, a.scale_log2);
+            } else {
+                attend_tile<D, false, TREE>(raw, shared.stage[wave], q, state, lane, seq.length, limit, 0, a.scale_log2);
+            }
         };
         // kHeld - 1 tiles ahead, in registers that are not copied
         if (count > 0) {
@@ -821,19 +717,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
     }
 }
 
-gqsa_status_t on_device(const gqsa_cache* c)
-{
-    int dev = -1;
-    GQSA_HIP(hipGetDevice(&dev));
-    if (dev != c->device) return GQSA_ERR_HIP;
-    return GQSA_OK;
-}
-
-Pool pool_of(const gqsa_cache* c)
-{
-    return {c->d_pages, c->n_pages, __builtin_ctz(static_cast<unsigned>(c->page_tokens)), c->kv_heads};
-}
-
 }  // namespace
 
 gqsa_status_t cache_allocate(gqsa_cache* c)
@@ -862,12 +745,6 @@ void cache_release(gqsa_cache* c)
     c->d_arrivals = nullptr;
 }
 
-// Units of a copy: no more than a tile for every 32 rows and two more for every sequence.
-static dim3 copy_grid(const gqsa_cache* c, const Sequences& s)
-{
-    return dim3(static_cast<unsigned>(s.n_rows / kTileTokens + 2 * int64_t{s.n_seqs}), static_cast<unsigned>(c->kv_heads));
-}
-
 gqsa_status_t cache_append(gqsa_cache* c, const Heads& k, const Heads& v, const Sequences& seqs, void* stream)
 {
     if (gqsa_status_t st = on_device(c)) return st;
@@ -890,25 +767,41 @@ gqsa_status_t cache_read(gqsa_cache* c, const Heads& k, const Heads& v, const Se
     return GQSA_OK;
 }
 
-gqsa_status_t cache_attend(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, float scale, const Heads& out, void* stream)
+static gqsa_status_t attend(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, const uint32_t* masks, int mask_words, float scale,
+                            const Heads& out, void* stream)
 {
     if (gqsa_status_t st = on_device(c)) return st;
     const int per = q_heads / c->kv_heads;
     const AttendArgs a{pool_of(c), q, out, seqs, c->d_partials, c->d_arrivals, per,
                        // (not 0, so that a masked score stays -infinity: 1e-30 leaves every weight at 1)
-                       std::max(std::fabs(scale) * 1.44269504088896341f, 1e-30f), scale < 0.0f};
+                       std::max(std::fabs(scale) * 1.44269504088896341f, 1e-30f), scale < 0.0f, masks, mask_words};
     // No more workgroups than there can be steps.  (The kernel counts them, and rows of a group, in 32 bits.)
     if (seqs.n_rows * per > (1 << 30)) return GQSA_ERR_SHAPE;
     const double blocks = (static_cast<double>(seqs.n_rows) * per / kRowBlock + seqs.n_seqs) * c->kv_heads;
     const double steps = blocks * (static_cast<double>(seqs.max_pages) * c->page_tokens / (kAttendWaves * kTileTokens) + 1.0);
     if (steps > INT_MAX) return GQSA_ERR_SHAPE;
-    const unsigned grid = static_cast<unsigned>(std::max(1.0, std::min<double>(kAttendWorkgroups, steps)));
+    const dim3 grid(static_cast<unsigned>(std::max(1.0, std::min<double>(kAttendWorkgroups, steps)))), threads(64 * kAttendWaves);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 threads(64 * kAttendWaves);
-    if (c->head_dim == 128) hipLaunchKernelGGL((attend_kernel<128, kAttendWaves>), dim3(grid), threads, 0, s, a);
-    else hipLaunchKernelGGL((attend_kernel<64, kAttendWaves>), dim3(grid), threads, 0, s, a);
+    if (masks) {
+        if (c->head_dim == 128) hipLaunchKernelGGL((attend_kernel<128, kAttendWaves, true>), grid, threads, 0, s, a);
+        else hipLaunchKernelGGL((attend_kernel<64, kAttendWaves, true>), grid, threads, 0, s, a);
+    } else {
+        if (c->head_dim == 128) hipLaunchKernelGGL((attend_kernel<128, kAttendWaves, false>), grid, threads, 0, s, a);
+        else hipLaunchKernelGGL((attend_kernel<64, kAttendWaves, false>), grid, threads, 0, s, a);
+    }
     GQSA_HIP(hipGetLastError());
     return GQSA_OK;
+}
+
+gqsa_status_t cache_attend(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, float scale, const Heads& out, void* stream)
+{
+    return attend(c, q, q_heads, seqs, nullptr, 0, scale, out, stream);
+}
+
+gqsa_status_t cache_attend_tree(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, const uint32_t* masks, int mask_words, float scale,
+                                const Heads& out, void* stream)
+{
+    return attend(c, q, q_heads, seqs, masks, mask_words, scale, out, stream);
 }
 
 }  // namespace gqsa

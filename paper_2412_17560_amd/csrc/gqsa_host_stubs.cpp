@@ -6,6 +6,7 @@
 #include "gqsa_attention.hpp"
 #include "gqsa_bench.h"
 #include "gqsa_internal.hpp"
+#include "gqsa_verify.hpp"
 
 namespace gqsa {
 
@@ -24,6 +25,12 @@ void cache_release(gqsa_cache*) {}
 gqsa_status_t cache_append(gqsa_cache*, const Heads&, const Heads&, const Sequences&, void*) { return GQSA_ERR_HIP; }
 gqsa_status_t cache_read(gqsa_cache*, const Heads&, const Heads&, const Sequences&, void*) { return GQSA_ERR_HIP; }
 gqsa_status_t cache_attend(gqsa_cache*, const Heads&, int, const Sequences&, float, const Heads&, void*) { return GQSA_ERR_HIP; }
+gqsa_status_t cache_append_rotated(gqsa_cache*, const RotateCall&, const Heads&, const Sequences&, void*) { return GQSA_ERR_HIP; }
+gqsa_status_t cache_attend_tree(gqsa_cache*, const Heads&, int, const Sequences&, const uint32_t*, int, float, const Heads&, void*) { return GQSA_ERR_HIP; }
+gqsa_status_t cache_keep(gqsa_cache*, const Sequences&, const int32_t*, const int32_t*, void*) { return GQSA_ERR_HIP; }
+gqsa_status_t verifier_allocate(gqsa_verifier*) { return GQSA_ERR_HIP; }
+void verifier_release(gqsa_verifier*) {}
+gqsa_status_t verify(gqsa_verifier*, const VerifyCall&, void*) { return GQSA_ERR_HIP; }
 gqsa_status_t prompt_attend(const PromptCall&, void*) { return GQSA_ERR_HIP; }
 
 }  // namespace gqsa

@@ -1,0 +1,628 @@
+"""A decoding step of several drafted tokens over the 4-bit cache -- append with norm and rotation on the way, attention of a tree's rows, verification, the accepted
+rows kept -- against the definitions in float64, on the GPU."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import paper_2412_17560_amd as gq
+from oracle import attention as ref
+from oracle import drafts
+from test_attention_gpu import Cached, _check_attended, _table, dev, ints, normal
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def starts_of(counts):
+    return np.cumsum([0] + list(counts)).astype(np.int32)
+
+
+def same(a, b):
+    """Equal, NaN to NaN."""
+    return a.shape == b.shape and np.array_equal(np.isnan(a), np.isnan(b)) and np.array_equal(np.nan_to_num(a), np.nan_to_num(b))
+
+
+# ----------------------------------------------------------------------------- append with norm and rotation
+def _append_rotated(c, counts, q_heads, rotary, interleaved, norm, *, positions=None, wide=1.0, k_out=True, eps=1e-5):
+    """Appends rows with planted sizes; checks queries, keys and what the cache then holds, bit for bit."""
+    n = sum(counts)
+    q, k, v = normal(c.rng, n, q_heads, c.dim) * np.float16(wide), c.some(n), c.some(n)
+    weights = [normal(c.rng, c.dim) if norm else None for _ in range(2)]
+    before = c.lengths()
+    place = np.concatenate([np.arange(b, b + m) for b, m in zip(before, counts)]).astype(np.int32)
+    table = _table(max(1, int(place.max(initial=0)) + 1 if positions is None else 97), rotary // 2) if rotary else None
+    at = place if positions is None else positions(c.rng, n)
+    starts = starts_of(counts)
+    out = torch.full((n, c.kv_heads, c.dim), 5.0, dtype=torch.float16, device="cuda") if k_out else None
+    got_q, got_k = gq.gqsa_cache_append_rotated(
+        c.cache, dev(q) if q_heads else None, dev(k), dev(v), None if positions is None or not rotary else dev(at), dev(table) if rotary else None, dev(c.pages),
+        ints(*[b + m for b, m in zip(before, counts)]), dev(starts), *[dev(w) if norm else None for w in weights], eps=eps, interleaved=interleaved, k_out=out)
+    kw = dict(positions=at, table=table, eps=eps, interleaved=interleaved)
+    want_k = drafts.norm_rotate_rounded(k, weight=weights[1], **kw)
+    if q_heads:
+        assert same(got_q.cpu().numpy(), drafts.norm_rotate_rounded(q, weight=weights[0], **kw))
+    if k_out:
+        assert same(got_k.cpu().numpy(), want_k)
+    c.k = [np.concatenate([a, want_k[s:e]]) for a, s, e in zip(c.k, starts, starts[1:])]
+    c.v = [np.concatenate([a, v[s:e]]) for a, s, e in zip(c.v, starts, starts[1:])]
+    c.check()
+
+
+@pytest.mark.parametrize("dim, page, q_heads, kv_heads, cached, counts, rotary, interleaved, norm", [
+    (128, 32, 1, 1, [0], [1], 128, False, True),                   # one token, an empty cache
+    (128, 64, 32, 32, [143], [1], 128, False, True),
+    (64, 32, 28, 4, [31, 0, 33], [1, 70, 40], 32, True, False),    # pairs side by side, half of the channels
+    (64, 32, 9, 3, [5, 60], [64, 4], 64, False, True),             # 9 query heads: two workgroups, the second with one
+    (128, 128, 8, 2, [100, 7, 0], [33, 0, 32], 96, False, True),   # partners a run apart that the group does not hold
+    (128, 32, 0, 5, [1], [31], 48, False, True),                   # no queries
+    (128, 32, 3, 1, [0], [200], 16, False, False),
+    (64, 64, 5, 5, [3], [17], 16, True, True),
+    (128, 32, 4, 4, [40], [3], 0, False, True),                    # norms only
+    (64, 256, 2, 1, [0], [300], 0, False, False),                  # neither
+    (128, 64, 16, 2, [0, 0, 0, 0], [5, 9, 16, 17], 128, True, True),
+])
+def test_append_rotated(dim, page, q_heads, kv_heads, cached, counts, rotary, interleaved, norm):
+    c = Cached(cached, kv_heads, dim, page, seed=dim + sum(counts), spare=2, room=max(counts) + 40)
+    _append_rotated(c, counts, q_heads, rotary, interleaved, norm)
+    _append_rotated(c, [2] * len(counts), q_heads, rotary, interleaved, norm, positions=lambda rng, n: rng.integers(0, 97, n).astype(np.int32), k_out=False)
+
+
+def test_append_rotated_without_norms_is_the_two_calls():
+    c, d = (Cached([20, 3], 2, 128, 32, seed=4, room=80) for _ in range(2))
+    counts, positions, table = [40, 1], np.arange(41, dtype=np.int32), _table(41, 64)
+    q, k, v = normal(c.rng, 41, 6, 128), c.some(41), c.some(41)
+    lengths, starts = ints(60, 4), dev(starts_of(counts))
+    rq, rk = gq.gqsa_qk_norm_rotate(dev(q), dev(k), dev(positions), dev(table))
+    gq.gqsa_cache_append(c.cache, rk, dev(v), dev(c.pages), lengths, starts)
+    oq, ok = gq.gqsa_cache_append_rotated(d.cache, dev(q), dev(k), dev(v), dev(positions), dev(table), dev(d.pages), lengths, starts, k_out=torch.empty_like(rk))
+    assert torch.equal(rq, oq) and torch.equal(rk, ok)
+    out = []
+    for x in (c, d):
+        out.append([torch.empty_like(rk) for _ in range(2)])
+        gq.gqsa_cache_read(x.cache, dev(x.pages), lengths, starts, *out[-1])
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_append_rotated_in_place_in_a_joint_array(interleaved):
+    c = Cached([10, 50], 2, 128, 32, seed=5, room=60)
+    counts, rows = [33, 20], 53
+    table, positions, weight = _table(64, 64), c.rng.integers(0, 64, rows).astype(np.int32), normal(c.rng, 128)
+    joint = normal(c.rng, rows, 12, 128)                                 # 8 query heads, 2 of keys, 2 of values
+    y = dev(joint)
+    lengths, starts = ints(43, 70), dev(starts_of(counts))
+    gq.gqsa_cache_append_rotated(c.cache, y[:, :8], y[:, 8:10], y[:, 10:], dev(positions), dev(table), dev(c.pages), lengths, starts, dev(weight), dev(weight),
+                                 interleaved=interleaved, q_out=y[:, :8], k_out=y[:, 8:10])
+    got = y.cpu().numpy()
+    kw = dict(positions=positions, table=table, weight=weight, interleaved=interleaved)
+    want = drafts.norm_rotate_rounded(joint[:, :10], **kw)
+    assert np.array_equal(got[:, :10], want) and np.array_equal(got[:, 10:], joint[:, 10:])
+    for b, (s, e) in enumerate(zip([0, 33], [33, 53])):
+        c.k[b], c.v[b] = np.concatenate([c.k[b], want[s:e, 8:]]), np.concatenate([c.v[b], joint[s:e, 10:]])
+    c.check()
+
+
+def test_append_rotated_heads_outermost_and_one_row_per_sequence():
+    c = Cached([31, 32, 0], 2, 64, 32, seed=3, room=1)
+    k, v, q = c.some(3), c.some(3), normal(c.rng, 3, 4, 64)
+    table = _table(40, 32)
+
+    def outermost(x):
+        return dev(x.transpose(1, 0, 2)).transpose(0, 1)
+    out, none = gq.gqsa_cache_append_rotated(c.cache, outermost(q), outermost(k), outermost(v), None, dev(table), dev(c.pages), ints(32, 33, 1))
+    assert none is None
+    kw = dict(positions=np.array([31, 32, 0]), table=table)
+    assert np.array_equal(out.cpu().numpy(), drafts.norm_rotate_rounded(q, **kw))
+    want = drafts.norm_rotate_rounded(k, **kw)
+    c.k, c.v = ([np.concatenate([x, new[b:b + 1]]) for b, x in enumerate(held)] for held, new in ((c.k, want), (c.v, v)))
+    c.check()
+
+
+def test_append_rotated_extremes():
+    """The largest and smallest numbers, zeros, infinities, NaN; positions outside the table."""
+    c = Cached([0], 1, 128, 32, room=64)
+    k, v = c.some(12), c.some(12)
+    k[0], k[1], k[2], k[3, 0, 7], k[4, 0, 9] = 65504, 6e-8, 0, np.inf, np.nan
+    v[5, 0, 3], v[6, 0, 64:96] = -np.inf, 2.5
+    weight, table = np.ones(128, np.float16), _table(9, 64)
+    positions = np.arange(12, dtype=np.int32)
+    positions[7], positions[8] = -1, 2 ** 30
+    q = k.copy()
+    out, ok = gq.gqsa_cache_append_rotated(c.cache, dev(q), dev(k), dev(v), dev(positions), dev(table), dev(c.pages), ints(12), ints(0, 12), dev(weight), dev(weight),
+                                           k_out=torch.empty((12, 1, 128), dtype=torch.float16, device="cuda"))
+    want = drafts.norm_rotate_rounded(k, positions=positions, table=table, weight=weight)
+    assert np.isnan(want[[4, 7, 8, 9, 10, 11]]).all() and np.isfinite(want[[0, 1, 2, 5, 6]]).all()
+    assert same(out.cpu().numpy(), want) and same(ok.cpu().numpy(), want)
+    c.k, c.v = [want], [v]
+    c.check()
+
+
+def test_rows_without_a_place_are_rotated_and_left_out():
+    """Below token 0, beyond the pages, on an absent page; rows of no sequence are not touched."""
+    c = Cached([40, 3], 1, 64, 32, seed=8, room=20)
+    held = [x.copy() for x in c.k[0:1] + c.v[0:1]]
+    n = 9
+    q, k, v, table = normal(c.rng, n, 2, 64), c.some(n), c.some(n), _table(200, 32)
+    pages = c.pages.copy()
+    pages[1, 0] = c.n_pages
+    room = torch.full((n, 2, 64), 7.0, dtype=torch.float16, device="cuda")
+    # sequence 0: rows 1 .. 3 would be tokens 62 .. 64, of which its two pages hold 62 and 63; sequence 1: rows 4 .. 7 would be tokens -2 .. 1, on an absent page
+    positions = np.arange(100, 109, dtype=np.int32)
+    gq.gqsa_cache_append_rotated(c.cache, dev(q), dev(k), dev(v), dev(positions), dev(table), dev(pages[:, :2]), ints(65, 2), ints(1, 4, 8), q_out=room)
+    got = room.cpu().numpy()
+    assert (got[[0, 8]] == 7).all()
+    assert np.array_equal(got[1:8], drafts.norm_rotate_rounded(q, positions=positions, table=table)[1:8])
+    want = drafts.norm_rotate_rounded(k, positions=positions, table=table)
+    kk, vv = (torch.empty((64, 1, 64), dtype=torch.float16, device="cuda") for _ in range(2))
+    gq.gqsa_cache_read(c.cache, dev(c.pages[:1]), ints(64), ints(0, 64), kk, vv)
+    assert np.array_equal(kk.cpu().numpy()[:40], ref.cache_values(held[0])) and np.array_equal(vv.cpu().numpy()[:40], ref.cache_values(held[1]))
+    assert np.array_equal(kk.cpu().numpy()[62:], ref.cache_values(want[1:3])) and np.array_equal(vv.cpu().numpy()[62:], ref.cache_values(v[1:3]))
+    c.k, c.v = [x[:0] for x in c.k[:1]] + c.k[1:], [x[:0] for x in c.v[:1]] + c.v[1:]
+    c.check()                                                            # the second sequence's tokens are as they were
+
+
+# ----------------------------------------------------------------------------- attention of a tree's rows
+def random_tree(rng, n, width):
+    return [-1] + [max(0, i - 1 - int(rng.integers(width))) for i in range(1, n)]
+
+
+def _attend_tree(c, sees, q_heads, scale=None, words=None, out=None):
+    """sees: per sequence bool [rows, rows]."""
+    counts = [len(s) for s in sees]
+    words = words or max(1, -(-max(counts) // 32))
+    masks = np.concatenate([drafts.mask_words(s, words).reshape(-1, words) for s in sees])
+    starts = starts_of(counts)
+    q = normal(c.rng, sum(counts), q_heads, c.dim)
+    out = torch.full((sum(counts), q_heads, c.dim), 9.0, dtype=torch.float16, device="cuda") if out is None else out
+    got = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(c.pages), ints(*c.lengths()), dev(starts), dev(masks), scale=scale, out=out)
+    assert got is out
+    y = out.cpu().numpy()
+    return [q[s:e] for s, e in zip(starts, starts[1:])], [y[s:e] for s, e in zip(starts, starts[1:])]
+
+
+def _check_tree(c, q, out, sees, scale=None):
+    for qb, got, k, v, s in zip(q, out, c.k, c.v, sees):
+        hk, hv = ref.cache_values(k), ref.cache_values(v)
+        want, size = drafts.tree_attention(qb, hk, hv, c.dim ** -0.5 if scale is None else scale, s)
+        _check_attended(got, want, size, len(k), hv)
+
+
+@pytest.mark.parametrize("dim, page, q_heads, kv_heads, lengths, counts, width", [
+    (128, 32, 1, 1, [1], [1], 1),
+    (128, 64, 32, 32, [151], [8], 3),                          # as many heads of keys as of queries
+    (64, 32, 28, 4, [100, 13, 300, 64], [13, 13, 1, 7], 4),    # a sequence of rows only
+    (128, 32, 8, 2, [95, 40, 33], [33, 40, 0], 5),             # more rows than a mask's word; rows across a tile's end; a sequence without rows
+    (128, 32, 8, 2, [500, 64], [64, 31], 8),
+    (64, 64, 7, 1, [700], [16], 3),                            # 112 rows over one head
+    (128, 128, 16, 1, [1000, 129], [64, 128], 16),             # 1024 and 2048 of them
+    (64, 32, 4, 4, [2500, 40], [100, 5], 9),
+    (128, 256, 64, 8, [5000], [16], 5),                        # split over the length
+    (128, 32, 40, 8, [3000, 20, 70], [6, 20, 50], 2),
+    (64, 32, 12, 12, [900], [17], 1),                          # a chain
+])
+def test_tree_attention(dim, page, q_heads, kv_heads, lengths, counts, width):
+    c = Cached(lengths, kv_heads, dim, page, seed=sum(lengths), spare=1)
+    sees = [drafts.ancestors(random_tree(c.rng, n, width)[:n]) for n in counts]
+    q, out = _attend_tree(c, sees, q_heads)
+    _check_tree(c, q, out, sees)
+    masks = np.concatenate([drafts.mask_words(s, -(-max(counts) // 32)) for s in sees])
+    again = gq.gqsa_cache_attend_tree(c.cache, dev(np.concatenate(q)), dev(c.pages), ints(*lengths), dev(starts_of(counts)), dev(masks)).cpu().numpy()
+    assert np.array_equal(again, np.concatenate(out))          # the same bits from run to run
+
+
+@pytest.mark.parametrize("q_heads, kv_heads, n, length", [(4, 2, 20, 20), (4, 2, 20, 333), (2, 2, 70, 71), (16, 1, 40, 90)])
+def test_rows_that_see_anything_of_each_other(q_heads, kv_heads, n, length):
+    """Masks that are no tree's: later rows, not themselves, nothing."""
+    c = Cached([length, length + 5], kv_heads, 128, 32, seed=n)
+    sees = [c.rng.random((n, n)) < 0.3 for _ in range(2)]
+    sees[0][3] = sees[1][n - 1] = False
+    q, out = _attend_tree(c, sees, q_heads)
+    if length == n:
+        assert (out[0][3] == 0).all()                          # nothing before it, nothing that it sees
+    _check_tree(c, q, out, sees)
+
+
+def test_more_words_than_rows_and_fewer():
+    c = Cached([90, 50], 1, 64, 32, seed=2)
+    sees = [drafts.ancestors(random_tree(c.rng, n, 3)) for n in (40, 9)]
+    q, out = _attend_tree(c, sees, 2, words=5)
+    _check_tree(c, q, out, sees)
+    q, out = _attend_tree(c, sees, 2, words=1)
+    sees[0][:, 32:] = False
+    _check_tree(c, q, out, sees)
+
+
+def test_bits_of_rows_that_a_sequence_does_not_have():
+    c = Cached([70, 40], 1, 64, 32, seed=3)
+    sees = [np.ones((5, 64), bool), np.ones((2, 64), bool)]
+    q, out = _attend_tree(c, sees, 2, words=2)
+    _check_tree(c, q, out, [s[:, :len(s)] for s in sees])
+
+
+def test_a_chains_masks_are_causal():
+    c = Cached([300, 77], 2, 128, 32, seed=6)
+    counts = [5, 2]
+    sees = [np.tri(n, dtype=bool) for n in counts]
+    q, out = _attend_tree(c, sees, 8)
+    causal = gq.gqsa_cache_attend(c.cache, dev(np.concatenate(q)), dev(c.pages), ints(300, 77), dev(starts_of(counts))).cpu().numpy()
+    for got, qb, k, v in zip(np.split(causal, [5]), q, c.k, c.v):
+        want, size = ref.attention(qb, ref.cache_values(k), ref.cache_values(v), 128 ** -0.5, [len(k) - len(qb) + i + 1 for i in range(len(qb))])
+        _check_attended(got, want, size, len(k), v)
+    _check_tree(c, q, out, sees)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+def test_tree_scales(scale):
+    c = Cached([200, 33], 2, 64, 32, seed=9)
+    sees = [drafts.ancestors(random_tree(c.rng, n, 3)) for n in (20, 33)]
+    q, out = _attend_tree(c, sees, 4, scale=scale)
+    _check_tree(c, q, out, sees, scale)
+
+
+def test_tree_attention_over_many_sequences():
+    lengths = [1 + (7 * b) % 90 for b in range(150)]
+    counts = [min(n, b % 7) for b, n in enumerate(lengths)]
+    c = Cached(lengths, 1, 64, 32, seed=4)
+    sees = [drafts.ancestors(random_tree(c.rng, n, 2)[:n]) for n in counts]
+    q, out = _attend_tree(c, sees, 6)
+    _check_tree(c, q, out, sees)
+
+
+@pytest.mark.parametrize("n", [3, 40])
+def test_what_a_row_does_not_see_does_not_matter(n):
+    """NaN in tokens behind the last one, and in rows that others see."""
+    c = Cached([0], 2, 128, 64, seed=6, room=192)
+    wild = c.some(192)
+    wild[60:] = np.nan
+    gq.gqsa_cache_append(c.cache, dev(wild), dev(wild), dev(c.pages), ints(192), ints(0, 192))
+    k, v = c.some(70 + n), c.some(70 + n)
+    v[70 + 1, 0, 40] = np.inf                                  # row 1: its group of values is NaN
+    k[70 + 2, 1, 3] = np.nan                                   # row 2, the other head: its scores are
+    c.append([k], [v])
+    sees = drafts.ancestors([-1] + [0] * (n - 1))
+    sees[:, 1:3] &= np.eye(n, dtype=bool)[:, 1:3]
+    q, (out,) = _attend_tree(c, [sees], 8)
+    rest = [i for i in range(n) if i not in (1, 2)]
+    assert np.isfinite(out[rest]).all()
+    assert np.isnan(out[1, :4, 32:64]).all() and np.isfinite(np.delete(out[1, :4], np.arange(32, 64), axis=1)).all() and np.isfinite(out[1, 4:]).all()
+    assert np.isfinite(out[2, :4]).all() and np.isnan(out[2, 4:]).all()
+    finite = [np.where(np.isfinite(x), x, 0) for x in (c.k[0], c.v[0])]
+    want, size = drafts.tree_attention(q[0], *map(ref.cache_values, finite), 128 ** -0.5, sees)
+    _check_attended(out[rest], want[rest], size[rest], 70 + n, finite[1])
+
+
+@pytest.mark.parametrize("n", [2, 50])
+def test_infinite_queries_of_a_tree(n):
+    c = Cached([90], 1, 64, 32, seed=16)
+    sees = drafts.ancestors(random_tree(c.rng, n, 2))
+    q = normal(c.rng, n, 3, 64)
+    q[0, 0, 5], q[1, 1, 9] = np.inf, -np.inf
+    out = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(c.pages), ints(90), ints(0, n), dev(drafts.mask_words(sees, 2))).cpu().numpy()
+    assert np.isnan(out[0, 0]).all() and np.isnan(out[1, 1]).all()
+    want, size = drafts.tree_attention(np.where(np.isinf(q), 0, q), ref.cache_values(c.k[0]), ref.cache_values(c.v[0]), 0.125, sees)
+    fine = np.ones((n, 3), bool)
+    fine[0, 0] = fine[1, 1] = False
+    _check_attended(out[fine], want[fine], size[fine], 90, c.v[0])
+
+
+@pytest.mark.parametrize("n", [2, 40])
+def test_absent_pages_are_absent_tokens_of_a_tree(n):
+    c = Cached([300], 2, 64, 32, seed=5)
+    c.pages[0, 2], c.pages[0, 5] = -1, c.n_pages
+    there = np.ones(300, bool)
+    there[64:96] = there[160:192] = False
+    sees = drafts.ancestors(random_tree(c.rng, n, 3))
+    q, (out,) = _attend_tree(c, [sees], 4)
+    want, size = drafts.tree_attention(q[0], ref.cache_values(c.k[0][there]), ref.cache_values(c.v[0][there]), 0.125, sees)
+    _check_attended(out, want, size, 300, c.v[0])
+    c.pages[:] = -1
+    _, (out,) = _attend_tree(c, [sees], 4)
+    assert (out == 0).all()
+
+
+@pytest.mark.parametrize("n", [6, 40])
+def test_more_rows_than_tokens_in_a_tree(n):
+    """The first rows have no token: nobody sees them; they see what their masks name."""
+    c = Cached([4], 1, 64, 32, seed=12)
+    sees = [np.tri(n, dtype=bool)]
+    q, (out,) = _attend_tree(c, sees, 2)
+    want, size = drafts.tree_attention(q[0], ref.cache_values(c.k[0]), ref.cache_values(c.v[0]), 0.125, sees[0])
+    assert (out[:n - 4] == 0).all()
+    _check_attended(out, want, size, 4, c.v[0])
+
+
+def test_a_trees_starts_and_lengths_beyond_their_arrays_stay_inside():
+    c = Cached([64, 64], 1, 64, 32, seed=11)
+    q = dev(normal(c.rng, 3, 2, 64))
+    room = torch.full((5, 2, 64), 4.0, dtype=torch.float16, device="cuda")
+    masks = dev(drafts.mask_words(np.ones((3, 3), bool), 1))
+    gq.gqsa_cache_attend_tree(c.cache, q, dev(c.pages), ints(10 ** 6, -3), ints(0, 2, 900), masks, out=room[1:4])
+    assert (room[0] == 4).all() and (room[4] == 4).all() and (room[3] == 0).all()
+    want, size = drafts.tree_attention(q[:2].cpu().numpy(), ref.cache_values(c.k[0]), ref.cache_values(c.v[0]), 0.125, np.ones((2, 2), bool))
+    _check_attended(room[1:3].cpu().numpy(), want, size, 64, c.v[0])
+    gq.gqsa_cache_attend_tree(c.cache, q, dev(c.pages), ints(64, 64), ints(-2 ** 31, 1, 2 ** 31 - 1), masks, out=room[1:4])
+    assert (room[0] == 4).all() and (room[4] == 4).all()
+
+
+@pytest.mark.parametrize("kv_heads, lengths, n", [(1, [70001], 3), (3, [33000], 24), (8, [16500], 5), (2, [300, 40000, 900], 20)])
+def test_a_trees_rows_over_many_workgroups(kv_heads, lengths, n):
+    """Equal weights, which are exact, and values that rise along the sequence: a part that is missing, or counted for another, shows."""
+    c = Cached([0] * len(lengths), kv_heads, 64, 1024, seed=len(lengths), room=max(lengths))
+    k, v = [c.some(m) for m in lengths], [c.some(m) for m in lengths]
+    for x in v:
+        x += (6 * np.linspace(-1, 1, len(x))[:, None, None] * np.arange(1, kv_heads + 1)[:, None]).astype(np.float16)
+    c.append(k, v)
+    sees = [drafts.ancestors(random_tree(c.rng, n, 4)) for _ in lengths]
+    for _ in range(3):                                         # (and leaves nothing behind for the next call)
+        q, out = _attend_tree(c, sees, 2 * kv_heads, scale=0.0)
+        for qb, got, kb, vb, s in zip(q, out, c.k, c.v, sees):
+            allowed = np.ones((n, len(vb)))
+            allowed[:, len(vb) - n:] = s
+            hv = ref.cache_values(vb).astype(np.float64)
+            want, size = (np.repeat(np.einsum("rt,thd->rhd", allowed, x), 2, axis=1) / allowed.sum(axis=1)[:, None, None] for x in (hv, np.abs(hv)))
+            assert (np.abs(got - want) <= (2.0 ** -11 + 2.0 ** -14) * size).all()
+
+
+def test_scores_of_a_tree_that_rise_and_fall_far():
+    c = Cached([0], 1, 128, 32, seed=2, room=1000)
+    k, v = c.some(1000), c.some(1000)
+    k *= (0.2 + 4.0 * np.abs(np.sin(np.arange(1000) / 50.0)))[:, None, None].astype(np.float16)
+    c.append([k], [v])
+    sees = [drafts.ancestors(random_tree(c.rng, 30, 4))]
+    q, out = _attend_tree(c, sees, 4, scale=0.5)
+    _check_tree(c, q, out, sees, 0.5)
+
+
+def test_strided_queries_and_results_of_a_tree():
+    c = Cached([100], 2, 128, 32, seed=8)
+    sees = drafts.ancestors(random_tree(c.rng, 20, 3))
+    joint = normal(c.rng, 20, 8, 128)
+    y = torch.zeros((4, 20, 128), dtype=torch.float16, device="cuda").transpose(0, 1)      # heads outermost
+    gq.gqsa_cache_attend_tree(c.cache, dev(joint)[:, 2:6], dev(c.pages), ints(100), ints(0, 20), dev(drafts.mask_words(sees, 1)), out=y)
+    _check_tree(c, [joint[:, 2:6]], [y.cpu().numpy()], [sees])
+
+
+# ----------------------------------------------------------------------------- rows kept
+def _check_kept(c, counts, paths, accepted, pages=None):
+    starts = starts_of(counts)
+    path = np.full(int(starts[-1]), -1, np.int32)
+    for s, p in zip(starts, paths):
+        path[s:s + len(p)] = p
+    gq.gqsa_cache_keep(c.cache, dev(c.pages if pages is None else pages), ints(*c.lengths()), dev(starts), dev(path), ints(*accepted))
+    for b, n in enumerate(counts):
+        if n:
+            of = len(c.k[b]) - n + np.array(drafts.kept(n, path[starts[b]:starts[b + 1]], accepted[b]))
+            for held in (c.k, c.v):
+                held[b] = np.concatenate([held[b][:len(held[b]) - n], held[b][of]])
+    if pages is None:
+        c.check()
+
+
+@pytest.mark.parametrize("dim, page, kv_heads, lengths, paths, counts", [
+    (128, 32, 1, [1], [[0]], [1]),
+    (128, 64, 4, [143], [[0, 2, 5, 7]], [8]),
+    (64, 32, 3, [35, 8, 64], [[0, 3, 4], [0], [0, 1, 2, 3]], [5, 8, 4]),                  # across a tile's end; nothing moves
+    (128, 32, 2, [70, 100], [[0, 1, 5, 30, 39], [0, 60, 61, 62, 63]], [40, 64]),          # from another tile, from another page
+    (64, 64, 2, [300], [list(range(0, 200, 2))], [200]),                                 # more than a tile is kept
+    (128, 32, 1, [90], [[0] + list(range(30, 80))], [85]),
+])
+def test_keep(dim, page, kv_heads, lengths, paths, counts):
+    c = Cached(lengths, kv_heads, dim, page, seed=sum(lengths), spare=1)
+    _check_kept(c, counts, paths, [len(p) - 1 for p in paths])
+
+
+def test_keep_leaves_out_what_it_cannot_take():
+    c = Cached([50, 40, 30], 2, 64, 32, seed=2)
+    # entries below their own place, beyond the rows, negative; more accepted than rows; nothing accepted; no rows
+    _check_kept(c, [6, 5, 0], [[0, 0, 9, -4, 5, 5], [2, 4, 4, 3, 4], []], [200, 4, 3])
+    _check_kept(c, [6, 5, 2], [[1, 2, 3, 4, 5, 5], [4, 4, 4, 4, 4], [1, 1]], [-1, -7, 0])
+
+
+def test_keep_on_absent_pages_and_below_token_0():
+    c = Cached([80, 5], 1, 64, 32, seed=3)
+    held = [x.copy() for x in c.k + c.v]
+    pages = c.pages.copy()
+    pages[0, 2] = -1                                            # tokens 64 .. 79
+    # rows 0 .. 39 of the first are tokens 40 .. 79: of its entries the second lies on the absent page, the third does not; rows 0 .. 7 of the second are tokens -3 .. 4
+    starts, path = starts_of([40, 8]), np.full(48, -1, np.int32)
+    path[:3], path[40:44] = [5, 30, 10], [1, 4, 5, 7]
+    gq.gqsa_cache_keep(c.cache, dev(pages), ints(80, 5), dev(starts), dev(path), ints(2, 3))
+    c.k[0], c.v[0] = held[0].copy(), held[2].copy()
+    for x, old in ((c.k, held[0]), (c.v, held[2])):
+        x[0][40], x[0][42] = old[45], old[50]
+    for x, old in ((c.k, held[1]), (c.v, held[3])):
+        x[1][0] = old[4]                                        # (row 3: token 0, from row 7: token 4)
+    c.check()
+
+
+def test_keep_carries_values_that_are_not_finite():
+    c = Cached([0], 1, 64, 32, room=40)
+    k, v = c.some(40), c.some(40)
+    k[35, 0, 2], v[37, 0, 40] = np.inf, np.nan
+    c.append([k], [v])
+    _check_kept(c, [10], [[0, 5, 7]], [2])
+
+
+# ----------------------------------------------------------------------------- verification
+def probabilities(rng, rows, vocab, cut=False):
+    logits = rng.standard_normal((rows, vocab))
+    np.put_along_axis(logits, rng.integers(0, vocab, (rows, 6)), 6.0 + 4.0 * rng.random((rows, 6)), axis=1)
+    p = np.exp(logits - logits.max(axis=1, keepdims=True))
+    if cut:
+        p[p < 1e-3] = 0
+    return (p / p.sum(axis=1, keepdims=True)).astype(np.float32)
+
+
+def drafted(rng, counts, vocab, kind, width=3, cut=False):
+    """What a call takes, per sequence: (target, tokens, uniforms, parents or None, draft or None)."""
+    out = []
+    for n in counts:
+        target = probabilities(rng, n, vocab, cut)
+        parents = list(range(-1, n - 1)) if kind != "tree" else random_tree(rng, n, width)[:n]
+        draft, tokens = None, np.zeros(n, np.int32)
+        if kind == "drawn":
+            draft = (0.6 * target[parents] + 0.4 * probabilities(rng, n, vocab)).astype(np.float32) if n else target
+            tokens = np.array([rng.choice(vocab, p=d.astype(np.float64) / d.sum(dtype=np.float64)) for d in draft], np.int32).reshape(n)
+        else:
+            for i in range(1, n):
+                order = np.argsort(-target[parents[i]], kind="stable")
+                tokens[i] = order[min(vocab - 1, sum(p == parents[i] for p in parents[:i]) + (rng.random() < 0.2))]
+        out.append((target, tokens, rng.random(n, dtype=np.float32), np.array(parents, np.int32) if kind == "tree" else None, draft))
+    return out
+
+
+def _verify(verifier, sequences, finals, pad=0, starts=None):
+    """Everything in one call; rows of probabilities `pad` elements further apart than they are long."""
+    def rows(i, dtype, fill=None):
+        parts = [s[i] for s in sequences]
+        return None if any(p is None for p in parts) else np.concatenate(parts).astype(dtype)
+    target, draft = rows(0, np.float32), rows(4, np.float32)
+
+    def apart(x):
+        if x is None:
+            return None
+        wide = torch.full((x.shape[0], x.shape[1] + pad), float("nan"), device="cuda")
+        wide[:, :x.shape[1]] = dev(x)
+        return wide[:, :x.shape[1]]
+    starts = starts_of([len(s[1]) for s in sequences]) if starts is None else starts
+    parents = rows(3, np.int32)
+    path, out, accepted = gq.gqsa_verify(verifier, apart(target), dev(rows(1, np.int32)), dev(rows(2, np.float32)), dev(np.asarray(finals, np.float32)), dev(starts),
+                                         parents=None if parents is None else dev(parents), draft=apart(draft))
+    return path.cpu().numpy(), out.cpu().numpy(), accepted.cpu().numpy()
+
+
+def _check_verified(sequences, finals, got):
+    path, out, accepted = got
+    at = 0
+    for b, (target, tokens, uniforms, parents, draft) in enumerate(sequences):
+        n = len(tokens)
+        if n == 0:
+            assert accepted[b] == -1
+            continue
+        way, drawn = drafts.verify(target, tokens, uniforms, np.float32(finals[b]), parents, draft)
+        rest = [-1] * (n - len(way))
+        assert accepted[b] == len(way) - 1
+        assert list(path[at:at + n]) == way + rest
+        assert list(out[at:at + n]) == [tokens[i] for i in way[1:]] + [drawn] + rest
+        at += n
+
+
+@pytest.mark.parametrize("kind", ["chain", "tree", "drawn"])
+@pytest.mark.parametrize("counts, vocab, pad", [
+    ([1], 7, 0), ([5], 1000, 0), ([4, 1, 0, 9], 4097, 3), ([6] * 40, 333, 1), ([64, 33, 2], 2000, 0), ([130], 501, 2), ([5, 7], 20001, 0)])
+def test_verify(kind, counts, vocab, pad):
+    rng = np.random.default_rng(vocab + len(counts))
+    verifier = gq.gqsa_verify_create(len(counts), vocab)
+    for cut in (False, True):
+        sequences, finals = drafted(rng, counts, vocab, kind, cut=cut), rng.random(len(counts), dtype=np.float32)
+        got = _verify(verifier, sequences, finals, pad)
+        _check_verified(sequences, finals, got)
+        again = _verify(verifier, sequences, finals, pad)
+        assert all(np.array_equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_verify_every_border(drawn):
+    """Probabilities that are exact, and a last number on each border and just below: the first token whose sum passes it."""
+    vocab = 4096 + 64
+    p = np.zeros((2, vocab), np.float32)
+    at = [0, 1, 5, 255, 256, 1023, 1024, 4095, 4096, 4097, vocab - 1]
+    p[:, at] = [2.0 ** -3] * 4 + [2.0 ** -4] * 6 + [2.0 ** -3]
+    draft = np.zeros_like(p)
+    draft[1, 0], draft[1, 5] = 1.0, 2.0 ** -4                    # token 0 was drawn and does not stand; half of token 5's is left
+    sums, finals = np.cumsum(p[0, at].astype(np.float64)), []
+    if drawn:
+        left = np.maximum(p[0, at].astype(np.float64) - draft[1, at], 0)
+        sums = np.cumsum(left) / 0.8125
+    for s in sums:
+        finals += [np.float32(s), np.nextafter(np.float32(s), np.float32(0))]
+    finals += [0.0, 1.0, 7.0, -1.0, np.nan]
+    n = len(finals)
+    sequences = [(p, np.array([0, 0], np.int32), np.array([0, 0.5], np.float32), None, draft) if drawn else
+                 (p[:1], np.zeros(1, np.int32), np.zeros(1, np.float32), None, None) for _ in range(n)]
+    verifier = gq.gqsa_verify_create(n, vocab)
+    _check_verified(sequences, finals, _verify(verifier, sequences, finals, pad=1))
+
+
+def test_verify_siblings_with_the_same_token_and_tokens_and_parents_outside():
+    rng = np.random.default_rng(3)
+    vocab, sequences = 50, []
+    for _ in range(60):
+        n = 12
+        target = probabilities(rng, n, vocab)
+        parents = np.array([-1] + [int(rng.integers(-2, i + 2)) for i in range(1, n)], np.int32)      # (some are no parents)
+        parents = np.where(rng.random(n) < 0.5, np.where(np.arange(n) > 0, 0, -1), parents).astype(np.int32)
+        tokens = np.argsort(-target[0])[rng.integers(0, 4, n)].astype(np.int32)
+        tokens[rng.integers(1, n, 2)] = [-1, vocab]
+        sequences.append((target, tokens, rng.random(n, dtype=np.float32), parents, None))
+    clean = [(t, x, u, np.where(p < np.arange(len(p)), p, -1), None) for t, x, u, p, _ in sequences]
+    finals = rng.random(60, dtype=np.float32)
+    _check_verified(clean, finals, _verify(gq.gqsa_verify_create(60, vocab), sequences, finals))
+
+
+def test_verify_where_nothing_is_left():
+    """The children's probabilities are all there is, and none stands; draft and target alike; no probability at all; what is not a number."""
+    one, vocab = np.zeros((3, 5000), np.float32), 5000
+    one[:, [7, 4900]] = 0.5
+    stand = np.array([0.0, 1.0, 1.0], np.float32)                # (1 is not below 1: neither child stands)
+    sequences = [(one, np.array([0, 7, 4900], np.int32), stand, np.array([-1, 0, 0], np.int32), None)] * 3
+    nothing = np.zeros((2, vocab), np.float32)
+    odd = nothing.copy()
+    odd[0, :6] = [np.nan, np.inf, -np.inf, -0.5, 0.25, np.nan]
+    sequences += [(x, np.zeros(2, np.int32) + 4, np.array([0, 1], np.float32), np.array([-1, 0], np.int32), None) for x in (nothing, odd)]
+    sequences += [(x, np.zeros(2, np.int32) + 1, np.array([0, 0], np.float32), np.array([-1, 0], np.int32), None) for x in (nothing, odd)]
+    finals = [0.2, 0.5, 0.9, 0.5, 0.5, 0.5, 0.5]
+    got = _verify(gq.gqsa_verify_create(7, vocab), sequences, finals)
+    _check_verified(sequences, finals, got)
+    assert list(got[1][0:9:3]) == [7, 4900, 4900] and list(got[1][9:]) == [-1, -1, 4, -1, -1, -1, 4, -1]
+    alike = probabilities(np.random.default_rng(1), 3, 777)
+    alike[1:] = alike[0]
+    sequences = [(alike, np.array([0, 5, 6], np.int32), np.array([0, 1, 0], np.float32), None, alike)] * 2
+    finals = [0.3, 0.99]
+    _check_verified(sequences, finals, _verify(gq.gqsa_verify_create(2, 777), sequences, finals))
+
+
+def test_verify_rows_beyond_the_1024th_are_not_looked_at():
+    rng = np.random.default_rng(9)
+    n, vocab = 1100, 40
+    target = probabilities(rng, n, vocab)
+    tokens = np.concatenate([[0], target[:-1].argmax(axis=1)]).astype(np.int32)
+    (a, b), finals = [(target, tokens, np.zeros(n, np.float32), None, None), drafted(rng, [1024], vocab, "tree", 6)[0]], [0.4, 0.6]
+    verifier = gq.gqsa_verify_create(1, vocab)
+    path, out, accepted = _verify(verifier, [a], finals[:1])
+    assert accepted[0] == 1023 and list(path[:1024]) == list(range(1024)) and (path[1024:] == -1).all() and (out[1024:] == -1).all()
+    assert out[1023] == drafts.verify(*[x[:1024] if x is not None else None for x in a[:3]], 0.4)[1]
+    _check_verified([b], finals[1:], _verify(verifier, [b], finals[1:]))
+
+
+def test_verify_without_starts_draws_a_token_for_each_row():
+    rng = np.random.default_rng(2)
+    p, finals = probabilities(rng, 9, 10007), rng.random(9, dtype=np.float32)
+    verifier = gq.gqsa_verify_create(9, 10007)
+    path, out, accepted = gq.gqsa_verify(verifier, dev(p), ints(*[0] * 9), dev(finals), dev(finals))
+    assert (path.cpu().numpy() == 0).all() and (accepted.cpu().numpy() == 0).all()
+    assert list(out.cpu().numpy()) == [drafts.verify(p[i:i + 1], [0], [0], finals[i])[1] for i in range(9)]
+
+
+def test_verify_starts_beyond_the_rows_and_rows_of_no_sequence():
+    rng = np.random.default_rng(4)
+    sequences = drafted(rng, [3, 4, 3], 100, "tree")
+    target, tokens, uniforms, parents = (np.concatenate([s[i] for s in sequences]) for i in range(4))
+    path, out = (torch.full((10,), 77, dtype=torch.int32, device="cuda") for _ in range(2))
+    verifier = gq.gqsa_verify_create(4, 100)
+    _, _, accepted = gq.gqsa_verify(verifier, dev(target), dev(tokens), dev(uniforms), dev(np.array([0.1, 0.2, 0.3, 0.4], np.float32)), ints(3, 7, 7, 2 ** 31 - 1, -2 ** 31),
+                                    parents=dev(parents), path=path, out=out)
+    assert (path[:3] == 77).all() and (out[:3] == 77).all()
+    accepted = accepted.cpu().numpy()
+    assert accepted[1] == accepted[3] == -1
+    got = path[3:].cpu().numpy(), out[3:].cpu().numpy(), accepted[[0, 2]]
+    _check_verified(sequences[1:], [0.1, 0.3], got)
+
+
+def test_verify_a_large_vocabulary_and_a_handle_made_for_more():
+    rng = np.random.default_rng(6)
+    verifier = gq.gqsa_verify_create(8, 1 << 20)
+    for counts, vocab, kind in (([3, 2], 128256, "drawn"), ([5], 300007, "tree"), ([1] * 8, 17, "chain"), ([1], 1 << 20, "chain")):
+        sequences, finals = drafted(rng, counts, vocab, kind), rng.random(len(counts), dtype=np.float32)
+        _check_verified(sequences, finals, _verify(verifier, sequences, finals))
