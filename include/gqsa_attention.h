@@ -68,7 +68,7 @@ typedef struct {
     int32_t head_dim;
     int32_t token_bytes;        /* of one token and head: keys and values, codes, low and step */
     int64_t device_bytes;       /* pages */
-    int64_t workspace_bytes;    /* partial results of gqsa_cache_attend */
+    int64_t workspace_bytes;    /* partial results of gqsa_cache_attend and gqsa_cache_attend_tree: about 34 MB with heads of 128, half of that with 64 */
 } gqsa_cache_info_t;
 
 /*

@@ -19,7 +19,7 @@ SANITIZED_LIB = os.path.join(OBJ, "libgqsa_host_asan.so")
 # group sizes -- "file:part")
 SOURCES = ["gqsa_gemv.hip", *(f"gqsa_gemv.hip:{part}" for part in range(1, 9)), "gqsa_pack.cpp", "gqsa_panels.cpp",
            "gqsa_api.cpp", "gqsa_panel_kernel.hip", "gqsa_pack_device.hip", "gqsa_baselines.hip",
-           "gqsa_attention_api.cpp", "gqsa_rotate.hip", "gqsa_cache.hip", "gqsa_cache_rows.hip", "gqsa_prompt.hip",
+           "gqsa_attention_api.cpp", "gqsa_rotate.hip", "gqsa_cache.hip", "gqsa_cache_rows.hip", "gqsa_tree.hip", "gqsa_prompt.hip",
            "gqsa_verify_api.cpp", "gqsa_verify.hip"]
 
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", CSRC,

@@ -44,6 +44,9 @@ constexpr int tile_bytes(int head_dim) { return kTileTokens * head_dim + 2 * kTi
 constexpr int kAttendWorkgroups = 512;      // the most workgroups of one attention over the cache: two to a compute unit
 constexpr int kRowBlock = 16;               // query rows (rows of a sequence times the heads of a group) per product
 
+constexpr int kTreeWorkgroups = 256;        // the most workgroups of one attention of trees: one to a compute unit
+constexpr int kTreeRows = 128;              // rows of a block there
+
 // The rows that a sequence has, from the two ends that an array on the device gives, which may be anything: none outside 0 .. n - 1 (n at most 2^25).  Both
 // ends are brought into 0 .. n before one is taken off the other, as their difference may not fit 32 bits.
 struct Rows {
@@ -71,11 +74,17 @@ struct gqsa_cache {
     int page_tokens = 0, kv_heads = 0, head_dim = 0;
     int device = -1;
     uint8_t* d_pages = nullptr;
-    float* d_partials = nullptr;    // partial results of up to kRowBlock rows: two of every workgroup, one of several together
+    float* d_partials = nullptr;    // partial results of up to kRowBlock rows: two of every workgroup, one of several together; or those of trees
     int32_t* d_arrivals = nullptr;  // two counters for every workgroup, zero between calls
 
     int64_t device_bytes() const { return n_pages * kv_heads * (page_tokens / gqsa::kTileTokens) * int64_t{gqsa::tile_bytes(head_dim)}; }
-    int64_t partial_floats() const { return int64_t{gqsa::kAttendWorkgroups} * 3 * gqsa::kRowBlock * (head_dim + 2); }
+    int64_t partial_floats() const
+    {
+        // (of trees two blocks of rows for every workgroup, and five numbers)
+        const int64_t few = int64_t{gqsa::kAttendWorkgroups} * 3 * gqsa::kRowBlock * (head_dim + 2);
+        const int64_t trees = int64_t{2} * gqsa::kTreeWorkgroups * gqsa::kTreeRows * (head_dim + 2) + gqsa::kTreeWorkgroups * 5;
+        return few > trees ? few : trees;
+    }
     int64_t workspace_bytes() const { return partial_floats() * 4 + int64_t{gqsa::kAttendWorkgroups} * 2 * 4; }
 };
 
@@ -91,6 +100,8 @@ gqsa_status_t cache_attend(gqsa_cache* c, const Heads& q, int q_heads, const Seq
 gqsa_status_t cache_append_rotated(gqsa_cache* c, const RotateCall& call, const Heads& v, const Sequences& seqs, void* stream);
 gqsa_status_t cache_attend_tree(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, const uint32_t* masks, int mask_words, float scale,
                                 const Heads& out, void* stream);
+gqsa_status_t tree_attend(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, const uint32_t* masks, int mask_words, float scale,
+                          const Heads& out, void* stream);
 gqsa_status_t cache_keep(gqsa_cache* c, const Sequences& seqs, const int32_t* path, const int32_t* accepted, void* stream);
 
 struct PromptCall {
