@@ -617,6 +617,16 @@ gqsa_status_t cache_read(gqsa_cache* c, const Heads& k, const Heads& v, const Se
     return GQSA_OK;
 }
 
+// How many steps there can be at most.  (The kernels count them, and rows of a group, in 32 bits.)
+static gqsa_status_t most_steps(const gqsa_cache* c, int q_heads, const Sequences& seqs, double* steps)
+{
+    const int per = q_heads / c->kv_heads;
+    if (seqs.n_rows * per > (1 << 30)) return GQSA_ERR_SHAPE;
+    const double blocks = (static_cast<double>(seqs.n_rows) * per / kRowBlock + seqs.n_seqs) * c->kv_heads;
+    *steps = blocks * (static_cast<double>(seqs.max_pages) * c->page_tokens / (kAttendWaves * kTileTokens) + 1.0);
+    return *steps > INT_MAX ? GQSA_ERR_SHAPE : GQSA_OK;
+}
+
 static gqsa_status_t attend(gqsa_cache* c, const Heads& q, int q_heads, const Sequences& seqs, const uint32_t* masks, int mask_words, float scale,
                             const Heads& out, void* stream)
 {
@@ -625,11 +635,8 @@ static gqsa_status_t attend(gqsa_cache* c, const Heads& q, int q_heads, const Se
     const AttendArgs a{pool_of(c), q, out, seqs, c->d_partials, c->d_arrivals, per,
                        // (not 0, so that a masked score stays -infinity: 1e-30 leaves every weight at 1)
                        std::max(std::fabs(scale) * 1.44269504088896341f, 1e-30f), scale < 0.0f, masks, mask_words};
-    // No more workgroups than there can be steps.  (The kernel counts them, and rows of a group, in 32 bits.)
-    if (seqs.n_rows * per > (1 << 30)) return GQSA_ERR_SHAPE;
-    const double blocks = (static_cast<double>(seqs.n_rows) * per / kRowBlock + seqs.n_seqs) * c->kv_heads;
-    const double steps = blocks * (static_cast<double>(seqs.max_pages) * c->page_tokens / (kAttendWaves * kTileTokens) + 1.0);
-    if (steps > INT_MAX) return GQSA_ERR_SHAPE;
+    double steps = 0.0;
+    if (gqsa_status_t st = most_steps(c, q_heads, seqs, &steps)) return st;
     const dim3 grid(static_cast<unsigned>(std::max(1.0, std::min<double>(kAttendWorkgroups, steps)))), threads(64 * kAttendWaves);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (masks) {
@@ -652,7 +659,16 @@ gqsa_status_t cache_attend_tree(gqsa_cache* c, const Heads& q, int q_heads, cons
                                 const Heads& out, void* stream)
 {
     if (gqsa_status_t st = on_device(c)) return st;
-    if (seqs.n_rows * (q_heads / c->kv_heads) <= int64_t{4 * kRowBlock} * seqs.n_seqs) return attend(c, q, q_heads, seqs, masks, mask_words, scale, out, stream);
+    // The kernel for many rows where there is much work: it costs some 20 us, as much again where few workgroups begin and end several blocks, and then a third of what this one costs
+    // for the same.  The host knows the lengths no better than by the room that the table has.  us of this one / the one for many, heads of 128 unless said, by the blocks of 16 rows times 32 tokens:
+    //   64 rows and more: 32 k: 16 x 1000 tokens, 128 rows of 8 heads 37 / 50; 4 x 2000, 64 rows of 32 heads 34 / 42; 16 k: 16 x 1000, 64 of 8 21 / 28; 6 k: 32768, 96 of 1 23 / 35;
+    //   56 k: 7 of up to 16003, 49 rows of 4 heads of 64 24 / 30; 80 k: 4 x 20000, 64 of 8 71 / 54; 120 k: 96 of 8 94 / 68; 266 k: 16 x 4160, 256 of 8 202 / 95; 131072, 128 of 8 166 / 101;
+    //   fewer: 40 k: 4 x 20000, 32 rows of 8 44 / 50; 16 k: 4 x 2000, 32 of 32 23 / 30.
+    const int64_t rows = seqs.n_rows * (q_heads / c->kv_heads), room = int64_t{seqs.max_pages} * c->page_tokens;
+    const double work = static_cast<double>((rows + kRowBlock - 1) / kRowBlock) * static_cast<double>(room / kTileTokens) * c->kv_heads;
+    if (rows <= int64_t{2 * kRowBlock} * seqs.n_seqs || work < 65536.0) return attend(c, q, q_heads, seqs, masks, mask_words, scale, out, stream);
+    double steps = 0.0;
+    if (gqsa_status_t st = most_steps(c, q_heads, seqs, &steps)) return st;
     return tree_attend(c, q, q_heads, seqs, masks, mask_words, scale, out, stream);
 }
 

@@ -42,8 +42,9 @@ __device__ __forceinline__ int opaque(int v)
 __device__ __forceinline__ uint32_t seen_of(const uint32_t* mask, int words, int from, int left)
 {
     const int w = from >> 5, shift = from & 31;
-    const auto word = [&](int i) { return i < 0 ? ~0u : i < words ? mask[i] : 0u; };
-    const uint64_t both = uint64_t{word(w + 1)} << 32 | word(w);
+    const uint32_t held[2] = {mask[min(max(w, 0), words - 1)], mask[min(max(w + 1, 0), words - 1)]};       // (no branches: the loads are under way together)
+    const auto word = [&](int i) { return w + i < 0 ? ~0u : w + i < words ? held[i] : 0u; };
+    const uint64_t both = uint64_t{word(1)} << 32 | word(0);
     return static_cast<uint32_t>(both >> shift) & (left >= 32 ? ~0u : (1u << max(left, 0)) - 1u);
 }
 

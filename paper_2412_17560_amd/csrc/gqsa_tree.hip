@@ -52,13 +52,14 @@ template <int D>
 __device__ __forceinline__ int key_at(int token, int run) { return token * D + 8 * (run ^ (D == 128 ? token & 15 : (token >> 1) & 7)); }
 __device__ __forceinline__ int value_at(int element, int quad) { return element * 32 + 8 * (quad ^ (element >> 2 & 3)); }
 
-// The token of a tile that row m of the first product's operand is: scores then lie as a word of value codes has its tokens.
-__device__ __forceinline__ int token_of_row(int m) { return (m & 7) | (m & 8) << 1 | (m & 16) >> 1; }
 
 __device__ __forceinline__ uint32_t lds_address(const void* p)
 {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) uint8_t*)p));
 }
+
+// The token of a tile that row m of the first product's operand is: scores then lie as a word of value codes has its tokens.
+__device__ __forceinline__ int token_of_row(int m) { return (m & 7) | (m & 8) << 1 | (m & 16) >> 1; }
 
 // Half a tile's codes (16 bytes a lane) and parameters (4 bytes a lane) of keys, or of values, straight into LDS.  Not before the wavefront's reads of what lies there have
 // returned, as they have where what they gave has been used.  (The wait states are for scalar registers that a vector instruction may have written just before, which the
@@ -180,24 +181,22 @@ __device__ __forceinline__ void put_values(const RawHalf<D>& raw, const Places<D
     lds_write(at.v_write + buffer + 1024 * u, join(c[0], c[1], c[2], c[3]));           // (16 elements further on)
 }
 
-// N operands from LDS and the N products that they go into, two at a time and the next two under way meanwhile (left alone, the compiler waits for every read where it has
-// issued it).  STAGES pieces of other work are done between the products, which leave the vector units free for most of their time.
+// N operands from LDS and the N products that they go into, with the next ones always under way (left alone, the compiler waits for every read where it has issued it).  The
+// first ones have been asked for before.  STAGES pieces of other work are done between the products, which leave the vector units free for most of their time.
+constexpr int kAhead = 2;
+
 template <int N, int STAGES, typename Read, typename Product, typename Aside>
-__device__ __forceinline__ void stream_operands(Read read, Product product, Aside aside)
+__device__ __forceinline__ void stream_operands(half8_t (&x)[2][kAhead], Read read, Product product, Aside aside)
 {
-    constexpr int kAtOnce = 2;
-    static_assert(N % kAtOnce == 0, "");
-    half8_t x[2][kAtOnce];
-#pragma unroll
-    for (int e = 0; e < kAtOnce; ++e) x[0][e] = read(e);
+    static_assert(N % kAhead == 0, "");
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        if (n % kAtOnce == 0 && n + kAtOnce < N) {
+        if (n % kAhead == 0 && n + kAhead < N) {
 #pragma unroll
-            for (int e = 0; e < kAtOnce; ++e) x[(n / kAtOnce + 1) & 1][e] = read(n + kAtOnce + e);
+            for (int e = 0; e < kAhead; ++e) x[(n / kAhead + 1) & 1][e] = read(n + kAhead + e);
         }
         __builtin_amdgcn_sched_barrier(0);
-        product(n, x[n / kAtOnce & 1][n % kAtOnce]);
+        product(n, x[n / kAhead & 1][n % kAhead]);
 #pragma unroll
         for (int i = n * STAGES / N; i < (n + 1) * STAGES / N; ++i) aside(i);
         __builtin_amdgcn_sched_barrier(0);
@@ -268,29 +267,36 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
             if (a.negate) q[i] = -q[i];
             q[i] += q[i] - q[i];        // (an infinity as NaN: it makes a row NaN, which scores of -infinity only would not)
         }
-        const uint32_t* mask = a.masks + int64_t{seq.start + row} * a.mask_words;
+        const uint32_t* mask = a.masks + int64_t{seq.start + static_cast<int>(token0 + (head0 + min(own, rows - 1)) / per)} * a.mask_words;
 
         float16_t out[D / 32];
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) out[d] = float16_t{};
         float top = kMinusInf, sum = 0.0f;
 
-        // The wavefront turns half of every fourth tile into numbers; lane i knows the page of the i-th of the next 64, so that no load waits for another.
+        // The wavefront turns half of every fourth tile into numbers; lane i knows where the i-th of the next 64 lies, so that no load waits for another.
         const int32_t* table = a.seqs.pages + int64_t{b} * a.seqs.max_pages;
         const int tiles = uniform(min((seq.length + kTileTokens - 1) / kTileTokens, to * kStepTiles));
         const int my_tile = wave >> 1, my_half = wave & 1, count = to - from;
         const Places<D> places(shared, opaque(lane), wave, kPieces * part, my_tile, my_half);
-        int page_of_lane = 0;
         // (always the same number of loads: past the end and for absent pages of some tile that is there)
         int next_first = -1, after_first = -1;         // of the tile that is turned into numbers in this step, and of the one after it; -1: absent
         const uint8_t* after_tile = nullptr;
+        uint32_t tile_of_lane[2] = {};
+        int first_of_lane = -1;
         const auto load_keys = [&](int i) {
-            const int tile = (from + i) * kStepTiles + my_tile;
-            if ((i & 63) == 0 && i < count) page_of_lane = opaque(table[max(min((from + i + lane) * kStepTiles + my_tile, tiles - 1), 0) >> (a.pool.page_shift - 5)]);
-            const int page = __builtin_amdgcn_readlane(page_of_lane, i & 63);
-            const bool there = i < count && tile < tiles && page >= 0 && page < a.pool.n_pages;
-            after_first = there ? tile * kTileTokens : -1;
-            after_tile = a.pool.tile<D>(there ? page : 0, head, tile);
+            if ((i & 63) == 0) {
+                const int tile = (from + i + opaque(lane)) * kStepTiles + my_tile;
+                const int page = table[max(min(tile, tiles - 1), 0) >> (a.pool.page_shift - 5)];
+                const bool there = tile < tiles && page >= 0 && page < a.pool.n_pages;
+                const uint64_t at = reinterpret_cast<uint64_t>(a.pool.tile<D>(there ? page : 0, head, tile));
+                tile_of_lane[0] = static_cast<uint32_t>(at), tile_of_lane[1] = static_cast<uint32_t>(at >> 32);
+                first_of_lane = there ? tile * kTileTokens : -1;
+                asm volatile("" : "+v"(tile_of_lane[0]), "+v"(tile_of_lane[1]), "+v"(first_of_lane));
+            }
+            const uint32_t low = __builtin_amdgcn_readlane(tile_of_lane[0], i & 63), high = __builtin_amdgcn_readlane(tile_of_lane[1], i & 63);
+            after_first = __builtin_amdgcn_readlane(first_of_lane, i & 63);
+            after_tile = reinterpret_cast<const uint8_t*>(uint64_t{high} << 32 | low);
             copy_half(lds_address(shared.raw[wave][0]), after_tile, places.codes, places.parameters);
         };
         const auto load_values = [&] { copy_half(lds_address(shared.raw[wave][1]), after_tile, places.codes + 16 * D, places.parameters + 4 * D); };
@@ -321,26 +327,44 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
         bool all_seen;
         half8_t p[2 * kPieces];
         float16_t s[kPieces] = {};
+        half8_t x[2][kAhead];
+        const auto key_operand = [&](int buffer, int n) {       // (run 2 i + half)
+            return lds_read<half8_t>(((places.k_read + buffer * Places<D>::kBuffer) ^ (32 * (n / kPieces))) + n % kPieces * Places<D>::kTile);
+        };
+        const auto value_operand = [&](int buffer, int n) {     // (32 elements further on)
+            const int i = n / (D / 32), d = n % (D / 32);
+            return lds_read<half8_t>(((places.v_read + buffer * Places<D>::kBuffer) ^ (32 * (i & 1))) + (i >> 1) * Places<D>::kTile + d * 2048);
+        };
         const auto score = [&](int buffer) {
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) x[0][e] = key_operand(buffer, e);
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                first[j] = shared.first[buffer][kPieces * part + j];       // (made uniform when it is needed)
+                s[j] = float16_t{};
+            }
+            stream_operands<D / 16 * kPieces, kStages>(x, [&](int n) { return key_operand(buffer, n); },
+                                                       [&](int n, half8_t k) { s[n % kPieces] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[n / kPieces], s[n % kPieces], 0, 0, 0); },
+                                                       put_keys_of(buffer ^ 1));
+        };
+        const auto ask_for_values = [&](int buffer) {
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) x[0][e] = value_operand(buffer, e);
+        };
+        const auto weigh = [&] {
             all_seen = true;
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
-                first[j] = uniform(shared.first[buffer][kPieces * part + j]);
+                first[j] = uniform(first[j]);
                 all_seen &= first[j] >= 0 && first[j] + kTileTokens <= before;
             }
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) s[j] = float16_t{};
-            const uint32_t at = buffer * Places<D>::kBuffer;
-            stream_operands<D / 16 * kPieces, kStages>(
-                [&](int n) { return lds_read<half8_t>(((places.k_read + at) ^ (32 * (n / kPieces))) + n % kPieces * Places<D>::kTile); },       // (run 2 i + half)
-                [&](int n, half8_t k) { s[n % kPieces] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[n / kPieces], s[n % kPieces], 0, 0, 0); }, put_keys_of(buffer ^ 1));
-        };
-        const auto weigh = [&] {
             // element r of s[j] is row r % 4 + 8 (r / 4) + 4 half of the operand
             if (!all_seen) {
 #pragma unroll
+                for (int j = 0; j < kPieces; ++j) seen[j] = seen_of(mask, a.mask_words, first[j] - before, seq.length - first[j]);
+#pragma unroll
                 for (int j = 0; j < kPieces; ++j) {
-                    seen[j] = is_row && first[j] >= 0 ? seen_of(mask, a.mask_words, first[j] - before, seq.length - first[j]) : 0u;
+                    if (!is_row || first[j] < 0) seen[j] = 0;
                     const uint32_t sees = seen[j] >> 4 * half;
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
@@ -376,13 +400,9 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
                 for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2(half2_t{p[i][e], p[i][e + 1]}, ones, sum, false);
         };
         const auto add_values = [&](int buffer) {
-            const uint32_t at = buffer * Places<D>::kBuffer;
-            stream_operands<2 * kPieces * (D / 32), kStages>(
-                [&](int n) {
-                    const int i = n / (D / 32), d = n % (D / 32);
-                    return lds_read<half8_t>(((places.v_read + at) ^ (32 * (i & 1))) + (i >> 1) * Places<D>::kTile + d * 2048);       // (32 elements further on)
-                },
-                [&](int n, half8_t v) { out[n % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[n / (D / 32)], out[n % (D / 32)], 0, 0, 0); }, put_values_of(buffer ^ 1));
+            stream_operands<2 * kPieces * (D / 32), kStages>(x, [&](int n) { return value_operand(buffer, n); },
+                                                             [&](int n, half8_t v) { out[n % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[n / (D / 32)], out[n % (D / 32)], 0, 0, 0); },
+                                                             put_values_of(buffer ^ 1));
             if (!all_seen) {
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j) {
@@ -406,18 +426,23 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
         load_keys(1);
         load_values();
         next_first = after_first;
+        fetch_keys();
         for (int i = 0; i < count; ++i) {
             __syncthreads();            // the step's tiles are there, and nobody reads the ones before any more
-            fetch_keys();
             if (active) score(i & 1);
             else every(put_keys_of(~i & 1));
             load_keys(i + 2);
-            if (active) weigh();
             fetch_values(~i & 1);
-            if (active) add_values(i & 1);
-            else every(put_values_of(~i & 1));
+            if (active) {
+                ask_for_values(i & 1);
+                weigh();
+                add_values(i & 1);
+            } else {
+                every(put_values_of(~i & 1));
+            }
             load_values();
             next_first = after_first;
+            fetch_keys();
         }
 
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (copies past the end may be under way)
@@ -426,8 +451,8 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
         constexpr int kFours = 4 * (D / 32), kShare = kFours / kParts;
         sum += __shfl_xor(sum, 32);
         __syncthreads();
-        const int late = opaque(lane);
-        const uint32_t fours = lds_address(&shared) + late * 16, states = lds_address(&shared) + kTreeWaves * (kParts - 1) * kShare * 1024 + late * 8;
+        const int l = opaque(lane);
+        const uint32_t fours = lds_address(&shared) + l * 16, states = lds_address(&shared) + kTreeWaves * (kParts - 1) * kShare * 1024 + l * 8;
         const auto four = [&](int f) { return float4_t{out[f / 4][4 * (f % 4)], out[f / 4][4 * (f % 4) + 1], out[f / 4][4 * (f % 4) + 2], out[f / 4][4 * (f % 4) + 3]}; };
         // (where part `giver` of a group leaves the f-th four for part `taker`)
         const auto place = [&](int giver, int taker, int f) {
@@ -469,22 +494,23 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
         if (is_row) {
             const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;       // (a row that sees nothing: all sums are 0)
             uint16_t* y = a.out.data + int64_t{seq.start + row} * a.out.row + q_head * a.out.head;
-            float* kept = a.partials + static_cast<int64_t>(2 * me + (from == 0 ? 1 : 0)) * kPartial + own * D;
+            float* kept = a.partials + static_cast<int64_t>(2 * me + (from == 0 ? 1 : 0)) * kPartial;
+            const int r = 32 * group + (l & 31);
 #pragma unroll
             for (int f = 0; f < kShare; ++f) {
                 const int at_four = part * kShare + f, column = 32 * (at_four / 4) + 8 * (at_four % 4) + 4 * half;
                 if (whole) *reinterpret_cast<half4_t*>(y + column) = __builtin_convertvector(mine[f] * inverse, half4_t);
-                else *reinterpret_cast<float4_t*>(kept + column) = mine[f];
+                else *reinterpret_cast<float4_t*>(kept + r * D + column) = mine[f];
             }
-            if (!whole && part == 0 && half == 0) *reinterpret_cast<float2_t*>(kept + kRows * D - own * D + 2 * own) = float2_t{highest, sum};
+            if (!whole && part == 0 && half == 0) *reinterpret_cast<float2_t*>(kept + kRows * D + 2 * r) = float2_t{highest, sum};
         }
         if (from == 0 && to < steps && threadIdx.x == 0) {      // (the last segment that the workgroup has, if any)
             const unsigned last = owner_of(at + steps - 1);
             a.splits[me] = {static_cast<int>(last - me) + 1, rows, seq.start + static_cast<int>(token0), static_cast<int>(head * per), static_cast<int>(head0)};
         }
-        __syncthreads();       // (LDS is free again)
         at += to - from;
         within += to - from;
+        if (at < end) __syncthreads();       // (LDS is free again)
     }
 }
 

@@ -167,15 +167,27 @@ def random_tree(rng, n, width):
     return [-1] + [max(0, i - 1 - int(rng.integers(width))) for i in range(1, n)]
 
 
-def _attend_tree(c, sees, q_heads, scale=None, words=None, out=None):
+def roomy_pages(c, rows):
+    """The table with room for so many tokens that many rows over a head of the cache are worth the kernel for many (65536 blocks of 16 rows times 32 tokens)."""
+    blocks = max(1, -(-rows // 16)) * c.kv_heads
+    wide = np.full((c.pages.shape[0], max(c.pages.shape[1], -(-65536 * 32 // (blocks * c.page)))), -1, np.int32)
+    wide[:, :c.pages.shape[1]] = c.pages
+    return wide
+
+
+roomy = pytest.mark.parametrize("room", [False, True])      # the kernel for few rows, or (from 33 rows a head on) for many
+
+
+def _attend_tree(c, sees, q_heads, scale=None, words=None, out=None, room=False):
     """sees: per sequence bool [rows, rows]."""
+    pages = roomy_pages(c, sum(len(s) for s in sees) * q_heads // c.kv_heads) if room else c.pages
     counts = [len(s) for s in sees]
     words = words or max(1, -(-max(counts) // 32))
     masks = np.concatenate([drafts.mask_words(s, words).reshape(-1, words) for s in sees])
     starts = starts_of(counts)
     q = normal(c.rng, sum(counts), q_heads, c.dim)
     out = torch.full((sum(counts), q_heads, c.dim), 9.0, dtype=torch.float16, device="cuda") if out is None else out
-    got = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(c.pages), ints(*c.lengths()), dev(starts), dev(masks), scale=scale, out=out)
+    got = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(pages), ints(*c.lengths()), dev(starts), dev(masks), scale=scale, out=out)
     assert got is out
     y = out.cpu().numpy()
     return [q[s:e] for s, e in zip(starts, starts[1:])], [y[s:e] for s, e in zip(starts, starts[1:])]
@@ -188,6 +200,7 @@ def _check_tree(c, q, out, sees, scale=None):
         _check_attended(got, want, size, len(k), hv)
 
 
+@roomy
 @pytest.mark.parametrize("dim, page, q_heads, kv_heads, lengths, counts, width", [
     (128, 32, 1, 1, [1], [1], 1),
     (128, 64, 32, 32, [151], [8], 3),                          # as many heads of keys as of queries
@@ -201,42 +214,46 @@ def _check_tree(c, q, out, sees, scale=None):
     (128, 32, 40, 8, [3000, 20, 70], [6, 20, 50], 2),
     (64, 32, 12, 12, [900], [17], 1),                          # a chain
 ])
-def test_tree_attention(dim, page, q_heads, kv_heads, lengths, counts, width):
+def test_tree_attention(dim, page, q_heads, kv_heads, lengths, counts, width, room):
     c = Cached(lengths, kv_heads, dim, page, seed=sum(lengths), spare=1)
     sees = [drafts.ancestors(random_tree(c.rng, n, width)[:n]) for n in counts]
-    q, out = _attend_tree(c, sees, q_heads)
+    q, out = _attend_tree(c, sees, q_heads, room=room)
     _check_tree(c, q, out, sees)
     masks = np.concatenate([drafts.mask_words(s, -(-max(counts) // 32)) for s in sees])
-    again = gq.gqsa_cache_attend_tree(c.cache, dev(np.concatenate(q)), dev(c.pages), ints(*lengths), dev(starts_of(counts)), dev(masks)).cpu().numpy()
+    pages = roomy_pages(c, sum(counts) * q_heads // kv_heads) if room else c.pages
+    again = gq.gqsa_cache_attend_tree(c.cache, dev(np.concatenate(q)), dev(pages), ints(*lengths), dev(starts_of(counts)), dev(masks)).cpu().numpy()
     assert np.array_equal(again, np.concatenate(out))          # the same bits from run to run
 
 
+@roomy
 @pytest.mark.parametrize("q_heads, kv_heads, n, length", [(4, 2, 20, 20), (4, 2, 20, 333), (2, 2, 70, 71), (16, 1, 40, 90)])
-def test_rows_that_see_anything_of_each_other(q_heads, kv_heads, n, length):
+def test_rows_that_see_anything_of_each_other(q_heads, kv_heads, n, length, room):
     """Masks that are no tree's: later rows, not themselves, nothing."""
     c = Cached([length, length + 5], kv_heads, 128, 32, seed=n)
     sees = [c.rng.random((n, n)) < 0.3 for _ in range(2)]
     sees[0][3] = sees[1][n - 1] = False
-    q, out = _attend_tree(c, sees, q_heads)
+    q, out = _attend_tree(c, sees, q_heads, room=room)
     if length == n:
         assert (out[0][3] == 0).all()                          # nothing before it, nothing that it sees
     _check_tree(c, q, out, sees)
 
 
-def test_more_words_than_rows_and_fewer():
+@roomy
+def test_more_words_than_rows_and_fewer(room):
     c = Cached([90, 50], 1, 64, 32, seed=2)
     sees = [drafts.ancestors(random_tree(c.rng, n, 3)) for n in (40, 9)]
-    q, out = _attend_tree(c, sees, 2, words=5)
+    q, out = _attend_tree(c, sees, 2, words=5, room=room)
     _check_tree(c, q, out, sees)
-    q, out = _attend_tree(c, sees, 2, words=1)
+    q, out = _attend_tree(c, sees, 2, words=1, room=room)
     sees[0][:, 32:] = False
     _check_tree(c, q, out, sees)
 
 
-def test_bits_of_rows_that_a_sequence_does_not_have():
+@roomy
+def test_bits_of_rows_that_a_sequence_does_not_have(room):
     c = Cached([70, 40], 1, 64, 32, seed=3)
     sees = [np.ones((5, 64), bool), np.ones((2, 64), bool)]
-    q, out = _attend_tree(c, sees, 2, words=2)
+    q, out = _attend_tree(c, sees, 40 if room else 2, words=2, room=room)
     _check_tree(c, q, out, [s[:, :len(s)] for s in sees])
 
 
@@ -252,25 +269,28 @@ def test_a_chains_masks_are_causal():
     _check_tree(c, q, out, sees)
 
 
+@roomy
 @pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
-def test_tree_scales(scale):
+def test_tree_scales(scale, room):
     c = Cached([200, 33], 2, 64, 32, seed=9)
     sees = [drafts.ancestors(random_tree(c.rng, n, 3)) for n in (20, 33)]
-    q, out = _attend_tree(c, sees, 4, scale=scale)
+    q, out = _attend_tree(c, sees, 4, scale=scale, room=room)
     _check_tree(c, q, out, sees, scale)
 
 
-def test_tree_attention_over_many_sequences():
+@roomy
+def test_tree_attention_over_many_sequences(room):
     lengths = [1 + (7 * b) % 90 for b in range(150)]
     counts = [min(n, b % 7) for b, n in enumerate(lengths)]
     c = Cached(lengths, 1, 64, 32, seed=4)
     sees = [drafts.ancestors(random_tree(c.rng, n, 2)[:n]) for n in counts]
-    q, out = _attend_tree(c, sees, 6)
+    q, out = _attend_tree(c, sees, 40 if room else 6, room=room)
     _check_tree(c, q, out, sees)
 
 
+@roomy
 @pytest.mark.parametrize("n", [3, 40])
-def test_what_a_row_does_not_see_does_not_matter(n):
+def test_what_a_row_does_not_see_does_not_matter(n, room):
     """NaN in tokens behind the last one, and in rows that others see."""
     c = Cached([0], 2, 128, 64, seed=6, room=192)
     wild = c.some(192)
@@ -282,7 +302,7 @@ def test_what_a_row_does_not_see_does_not_matter(n):
     c.append([k], [v])
     sees = drafts.ancestors([-1] + [0] * (n - 1))
     sees[:, 1:3] &= np.eye(n, dtype=bool)[:, 1:3]
-    q, (out,) = _attend_tree(c, [sees], 8)
+    q, (out,) = _attend_tree(c, [sees], 8, room=room)
     rest = [i for i in range(n) if i not in (1, 2)]
     assert np.isfinite(out[rest]).all()
     assert np.isnan(out[1, :4, 32:64]).all() and np.isfinite(np.delete(out[1, :4], np.arange(32, 64), axis=1)).all() and np.isfinite(out[1, 4:]).all()
@@ -292,13 +312,15 @@ def test_what_a_row_does_not_see_does_not_matter(n):
     _check_attended(out[rest], want[rest], size[rest], 70 + n, finite[1])
 
 
+@roomy
 @pytest.mark.parametrize("n", [2, 50])
-def test_infinite_queries_of_a_tree(n):
+def test_infinite_queries_of_a_tree(n, room):
     c = Cached([90], 1, 64, 32, seed=16)
     sees = drafts.ancestors(random_tree(c.rng, n, 2))
     q = normal(c.rng, n, 3, 64)
     q[0, 0, 5], q[1, 1, 9] = np.inf, -np.inf
-    out = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(c.pages), ints(90), ints(0, n), dev(drafts.mask_words(sees, 2))).cpu().numpy()
+    pages = roomy_pages(c, 3 * n) if room else c.pages
+    out = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(pages), ints(90), ints(0, n), dev(drafts.mask_words(sees, 2))).cpu().numpy()
     assert np.isnan(out[0, 0]).all() and np.isnan(out[1, 1]).all()
     want, size = drafts.tree_attention(np.where(np.isinf(q), 0, q), ref.cache_values(c.k[0]), ref.cache_values(c.v[0]), 0.125, sees)
     fine = np.ones((n, 3), bool)
@@ -306,30 +328,43 @@ def test_infinite_queries_of_a_tree(n):
     _check_attended(out[fine], want[fine], size[fine], 90, c.v[0])
 
 
+@roomy
 @pytest.mark.parametrize("n", [2, 40])
-def test_absent_pages_are_absent_tokens_of_a_tree(n):
+def test_absent_pages_are_absent_tokens_of_a_tree(n, room):
     c = Cached([300], 2, 64, 32, seed=5)
     c.pages[0, 2], c.pages[0, 5] = -1, c.n_pages
     there = np.ones(300, bool)
     there[64:96] = there[160:192] = False
     sees = drafts.ancestors(random_tree(c.rng, n, 3))
-    q, (out,) = _attend_tree(c, [sees], 4)
+    q, (out,) = _attend_tree(c, [sees], 4, room=room)
     want, size = drafts.tree_attention(q[0], ref.cache_values(c.k[0][there]), ref.cache_values(c.v[0][there]), 0.125, sees)
     _check_attended(out, want, size, 300, c.v[0])
     c.pages[:] = -1
-    _, (out,) = _attend_tree(c, [sees], 4)
+    _, (out,) = _attend_tree(c, [sees], 4, room=room)
     assert (out == 0).all()
 
 
+@roomy
 @pytest.mark.parametrize("n", [6, 40])
-def test_more_rows_than_tokens_in_a_tree(n):
+def test_more_rows_than_tokens_in_a_tree(n, room):
     """The first rows have no token: nobody sees them; they see what their masks name."""
     c = Cached([4], 1, 64, 32, seed=12)
     sees = [np.tri(n, dtype=bool)]
-    q, (out,) = _attend_tree(c, sees, 2)
+    q, (out,) = _attend_tree(c, sees, 2, room=room)
     want, size = drafts.tree_attention(q[0], ref.cache_values(c.k[0]), ref.cache_values(c.v[0]), 0.125, sees[0])
     assert (out[:n - 4] == 0).all()
     _check_attended(out, want, size, 4, c.v[0])
+
+
+def test_a_length_beyond_the_pages_that_are_there():
+    """The table has room for it, but no pages: the rows' own tokens are absent, and so is all but the first 64."""
+    c = Cached([64], 1, 64, 32, seed=13)
+    n = 40
+    pages = roomy_pages(c, n)
+    q = normal(c.rng, n, 1, 64)
+    out = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(pages), ints(1000), ints(0, n), dev(drafts.mask_words(np.ones((n, n), bool), 2))).cpu().numpy()
+    want, size = ref.attention(q, ref.cache_values(c.k[0]), ref.cache_values(c.v[0]), 0.125, [64] * n)
+    _check_attended(out, want, size, 64, c.v[0])
 
 
 def test_a_trees_starts_and_lengths_beyond_their_arrays_stay_inside():
@@ -345,8 +380,9 @@ def test_a_trees_starts_and_lengths_beyond_their_arrays_stay_inside():
     assert (room[0] == 4).all() and (room[4] == 4).all()
 
 
+@roomy
 @pytest.mark.parametrize("kv_heads, lengths, n", [(1, [70001], 3), (3, [33000], 24), (8, [16500], 5), (2, [300, 40000, 900], 20)])
-def test_a_trees_rows_over_many_workgroups(kv_heads, lengths, n):
+def test_a_trees_rows_over_many_workgroups(kv_heads, lengths, n, room):
     """Equal weights, which are exact, and values that rise along the sequence: a part that is missing, or counted for another, shows."""
     c = Cached([0] * len(lengths), kv_heads, 64, 1024, seed=len(lengths), room=max(lengths))
     k, v = [c.some(m) for m in lengths], [c.some(m) for m in lengths]
@@ -355,7 +391,7 @@ def test_a_trees_rows_over_many_workgroups(kv_heads, lengths, n):
     c.append(k, v)
     sees = [drafts.ancestors(random_tree(c.rng, n, 4)) for _ in lengths]
     for _ in range(3):                                         # (and leaves nothing behind for the next call)
-        q, out = _attend_tree(c, sees, 2 * kv_heads, scale=0.0)
+        q, out = _attend_tree(c, sees, 2 * kv_heads, scale=0.0, room=room)
         for qb, got, kb, vb, s in zip(q, out, c.k, c.v, sees):
             allowed = np.ones((n, len(vb)))
             allowed[:, len(vb) - n:] = s
@@ -364,22 +400,25 @@ def test_a_trees_rows_over_many_workgroups(kv_heads, lengths, n):
             assert (np.abs(got - want) <= (2.0 ** -11 + 2.0 ** -14) * size).all()
 
 
-def test_scores_of_a_tree_that_rise_and_fall_far():
+@roomy
+def test_scores_of_a_tree_that_rise_and_fall_far(room):
     c = Cached([0], 1, 128, 32, seed=2, room=1000)
     k, v = c.some(1000), c.some(1000)
     k *= (0.2 + 4.0 * np.abs(np.sin(np.arange(1000) / 50.0)))[:, None, None].astype(np.float16)
     c.append([k], [v])
     sees = [drafts.ancestors(random_tree(c.rng, 30, 4))]
-    q, out = _attend_tree(c, sees, 4, scale=0.5)
+    q, out = _attend_tree(c, sees, 4, scale=0.5, room=room)
     _check_tree(c, q, out, sees, 0.5)
 
 
-def test_strided_queries_and_results_of_a_tree():
+@roomy
+def test_strided_queries_and_results_of_a_tree(room):
     c = Cached([100], 2, 128, 32, seed=8)
     sees = drafts.ancestors(random_tree(c.rng, 20, 3))
     joint = normal(c.rng, 20, 8, 128)
     y = torch.zeros((4, 20, 128), dtype=torch.float16, device="cuda").transpose(0, 1)      # heads outermost
-    gq.gqsa_cache_attend_tree(c.cache, dev(joint)[:, 2:6], dev(c.pages), ints(100), ints(0, 20), dev(drafts.mask_words(sees, 1)), out=y)
+    pages = roomy_pages(c, 40) if room else c.pages
+    gq.gqsa_cache_attend_tree(c.cache, dev(joint)[:, 2:6], dev(pages), ints(100), ints(0, 20), dev(drafts.mask_words(sees, 1)), out=y)
     _check_tree(c, [joint[:, 2:6]], [y.cpu().numpy()], [sees])
 
 
