@@ -8,7 +8,7 @@
 
 namespace gqsa {
 
-constexpr int kVerifyChunk = 4096;      // of the vocabulary: a workgroup's share of a sequence
+constexpr int kVerifyChunk = 16384, kVerifyRun = 2048;      // of the vocabulary: a workgroup's share of a sequence, a wavefront's
 
 struct VerifyCall {
     const float *target, *draft;
@@ -26,10 +26,10 @@ struct VerifyCall {
 struct gqsa_verifier {
     int max_seqs = 0, max_vocab = 0;
     int device = -1;
-    double* d_sums = nullptr;       // of every chunk of every sequence
+    double* d_sums = nullptr;       // of every run of every sequence
     int32_t* d_arrivals = nullptr;  // a counter for every sequence, zero between calls
 
-    int64_t max_chunks() const { return int64_t{max_seqs} * ((int64_t{max_vocab} + gqsa::kVerifyChunk - 1) / gqsa::kVerifyChunk); }
+    int64_t max_runs() const { return int64_t{max_seqs} * ((int64_t{max_vocab} + gqsa::kVerifyRun - 1) / gqsa::kVerifyRun); }
 };
 
 namespace gqsa {
