@@ -109,7 +109,9 @@ struct RotatedArgs {
     float eps;
 };
 
-constexpr int kQueryHeads = 8;      // of one workgroup
+// Query heads of one workgroup: kQuerySets times what a wavefront takes of a row at once, 16 elements a lane; a wavefront takes one row.
+constexpr int kQuerySets = 2, kQueryRows = kThreads / 64;
+constexpr int query_heads_of(int head_dim) { return kQuerySets * 1024 / head_dim; }
 
 // 1 / sqrt(x) in 64 bits, from the hardware's estimate by one step (a start that is off by 2^-14 or less leaves 2^-27, two 2^-52; the estimate is far better),
 // and rounded to 32: a factor that does not depend on the order in which the squares were added.
@@ -121,161 +123,144 @@ __device__ __forceinline__ float root_of(double x)
     return static_cast<float>(x > 0.0 && x < __builtin_inf() ? z : y);
 }
 
-// N / 8 runs of 8 elements of a head from run `run0` on, normed and rotated; `x` its elements, `partner` those that they are rotated with.
-template <int N, bool INTERLEAVED>
-__device__ __forceinline__ void norm_rotate(half8_t (&x)[N / 8], const half8_t (&partner)[N / 8], const half8_t (&w)[N / 8], const half8_t (&w_partner)[N / 8], bool norm,
-                                            const float4_t (&turn)[N / 8][4], int run0, int turned, int head_dim, float eps)
-{
-    float factor = 1.0f;
-    if (norm) {
-        double sum = 0.0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const double v = static_cast<double>(static_cast<float>(x[i / 8][i % 8]));
-            sum = __builtin_fma(v, v, sum);
-        }
-#pragma unroll
-        for (int d = 1; d < 8; d *= 2) sum += __shfl_xor(sum, d);
-        factor = root_of(sum * (1.0 / head_dim) + static_cast<double>(eps));       // (head_dim is a power of two)
-    }
-#pragma unroll
-    for (int r = 0; r < N / 8; ++r) {
-        const bool turns = run0 + r < 2 * turned;
-        float own[8], other[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            own[i] = static_cast<float>(x[r][i]), other[i] = static_cast<float>(partner[r][i]);
-            if (norm) own[i] *= factor * static_cast<float>(w[r][i]), other[i] *= factor * static_cast<float>(w_partner[r][i]);
-        }
-        float y[8];
-        if constexpr (INTERLEAVED) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float c = turn[r][i / 2][2 * (i % 2)], s = turn[r][i / 2][2 * (i % 2) + 1], a = own[2 * i], b = own[2 * i + 1];
-                y[2 * i] = a * c - b * s, y[2 * i + 1] = a * s + b * c;
-            }
-        } else {
-            const bool first = run0 + r < turned;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float c = turn[r][i / 2][2 * (i % 2)], s = turn[r][i / 2][2 * (i % 2) + 1];
-                const float here = own[i] * c, there = other[i] * s;
-                y[i] = first ? here - there : there + here;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[r][i] = static_cast<_Float16>(turns ? y[i] : own[i]);
-    }
-}
-
-// What 8 threads to a token and head need for that: their own runs' partners, weights, cosines and sines.
+// The rotation of one token as D / 16 lanes need it: lane p has two runs of 8 elements of a head that are each other's partners, so that nothing is exchanged but the norm's sum.
 template <int D, bool INTERLEAVED>
-struct Rotation {
-    static constexpr int kOwn = D / 8, kRuns = kOwn / 8;
-    int run0, turned;
-    bool norm;
-    float eps;
-    int with[kRuns];            // the partners' runs
-    float4_t turn[kRuns][4];
-    half8_t w[kRuns], w_partner[kRuns];
+struct Turn {
+    static constexpr int kLanes = D / 16;
+    int run_a, run_b;
+    bool turns;
+    float4_t by[4];             // cosine and sine of the lane's 8 pairs
 
-    __device__ __forceinline__ Rotation(const RotatedArgs& a, const uint16_t* weight, int part, bool there, int64_t row, int token)
+    __device__ __forceinline__ Turn(const RotatedArgs& a, int p, bool there, int64_t row, int token)
     {
-        run0 = part * kRuns, turned = a.turned, norm = weight != nullptr, eps = a.eps;
-#pragma unroll
-        for (int r = 0; r < kRuns; ++r) {
-            const int run = run0 + r;
-            with[r] = INTERLEAVED || run >= 2 * turned ? run : run < turned ? run + turned : run - turned;
-            w[r] = w_partner[r] = half8_t{};
-            if (norm) w[r] = *reinterpret_cast<const half8_t*>(weight + 8 * run), w_partner[r] = *reinterpret_cast<const half8_t*>(weight + 8 * with[r]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) turn[r][i] = float4_t{};
-        }
-        if (turned == 0 || !there) return;
-        const int64_t position = a.positions ? a.positions[row] : token;
+        turns = p < a.turned;
+        run_a = INTERLEAVED || !turns ? 2 * p : p, run_b = INTERLEAVED || !turns ? 2 * p + 1 : p + a.turned;
+        if (!turns || !there) return;
+        const int position = a.positions ? a.positions[row] : token;
         const bool known = position >= 0 && position < a.n_positions;
-        const float* at = a.table + (known ? position : 0) * (16 * turned);
+        const float4_t* table = reinterpret_cast<const float4_t*>(a.table + (static_cast<int64_t>(known ? position : 0) * a.turned + p) * 16);
 #pragma unroll
-        for (int r = 0; r < kRuns; ++r) {
-            const int run = run0 + r;
-            if (run >= 2 * turned) continue;
-            // 8 pairs of the run, or, interleaved, 4
-            const float4_t* from = reinterpret_cast<const float4_t*>(at + (INTERLEAVED ? 8 * run : 16 * (run < turned ? run : run - turned)));
+        for (int i = 0; i < 4; ++i) {
+            by[i] = table[i];
+            if (!known) by[i] = __builtin_nanf("") + float4_t{};
+        }
+    }
+
+    struct Runs {
+        half8_t a, b;
+    };
+    __device__ __forceinline__ Runs load(const uint16_t* head) const { return {*reinterpret_cast<const half8_t*>(head + 8 * run_a), *reinterpret_cast<const half8_t*>(head + 8 * run_b)}; }
+    __device__ __forceinline__ void store(uint16_t* head, const Runs& x) const
+    {
+        *reinterpret_cast<half8_t*>(head + 8 * run_a) = x.a;
+        *reinterpret_cast<half8_t*>(head + 8 * run_b) = x.b;
+    }
+
+    // (called by all lanes of the head)
+    __device__ __forceinline__ Runs apply(const Runs& from, const uint16_t* weight, float eps) const
+    {
+        float x[2][8];
 #pragma unroll
-            for (int i = 0; i < (INTERLEAVED ? 2 : 4); ++i) {
-                turn[r][i] = from[i];
-                if (!known) turn[r][i] = __builtin_nanf("") + float4_t{};
+        for (int i = 0; i < 8; ++i) x[0][i] = static_cast<float>(from.a[i]), x[1][i] = static_cast<float>(from.b[i]);
+        if (weight) {
+            double sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const double v = static_cast<double>(x[i / 8][i % 8]);
+                sum = __builtin_fma(v, v, sum);
+            }
+#pragma unroll
+            for (int d = 1; d < kLanes; d *= 2) sum += __shfl_xor(sum, d);
+            const float factor = root_of(sum * (1.0 / D) + static_cast<double>(eps));
+            const Runs w = load(weight);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[0][i] *= factor * static_cast<float>(w.a[i]), x[1][i] *= factor * static_cast<float>(w.b[i]);
+        }
+        if (turns) {
+            if constexpr (INTERLEAVED) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float c = by[2 * r + i / 2][2 * (i % 2)], s = by[2 * r + i / 2][2 * (i % 2) + 1], u = x[r][2 * i], v = x[r][2 * i + 1];
+                        x[r][2 * i] = u * c - v * s, x[r][2 * i + 1] = u * s + v * c;
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float c = by[i / 2][2 * (i % 2)], s = by[i / 2][2 * (i % 2) + 1], u = x[0][i], v = x[1][i];
+                    x[0][i] = u * c - v * s, x[1][i] = u * s + v * c;
+                }
             }
         }
-    }
-
-    __device__ __forceinline__ void load(const uint16_t* head, half8_t (&x)[kRuns], half8_t (&partner)[kRuns]) const
-    {
+        Runs to;
 #pragma unroll
-        for (int r = 0; r < kRuns; ++r) {
-            x[r] = *reinterpret_cast<const half8_t*>(head + 8 * (run0 + r));
-            partner[r] = INTERLEAVED ? half8_t{} : *reinterpret_cast<const half8_t*>(head + 8 * with[r]);
-        }
-    }
-
-    __device__ __forceinline__ void apply(half8_t (&x)[kRuns], const half8_t (&partner)[kRuns]) const
-    {
-        norm_rotate<kOwn, INTERLEAVED>(x, partner, w, w_partner, norm, turn, run0, turned, D, eps);
+        for (int i = 0; i < 8; ++i) to.a[i] = static_cast<_Float16>(x[0][i]), to.b[i] = static_cast<_Float16>(x[1][i]);
+        return to;
     }
 };
 
-// One workgroup per tile that gets rows, and head of the cache or kQueryHeads query heads.  8 threads to a token: for keys and values as in the append without
-// rotation, for queries with as many tokens side by side as the tile gets and the rest of the threads on further heads.
+// One workgroup per tile that gets rows, and head of the cache: 8 threads to a token, which norm and rotate its key as Turn has it, hand it over by way of LDS to have a run of its
+// elements each, and quantise these; or per kQueryRows rows of a tile and several query heads.
 template <int D, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void append_rotated_kernel(RotatedArgs a)
 {
-    constexpr int kOwn = D / 8, kRuns = kOwn / 8;
+    constexpr int kOwn = D / 8, kRuns = kOwn / 8, kLanes = D / 16;
     __shared__ TileImage<D> shared;
+    __shared__ alignas(16) uint16_t keys[kTileTokens][D + 8];
     Unit u;
     if (!unit_of(a.copy, &u)) return;
     const int tile_token = u.tile * kTileTokens, first = u.seq.length - u.seq.rows - tile_token;       // the rows' first token, from the tile's on
     const int from = max(first, 0), to = min(u.seq.length - tile_token, kTileTokens);
-    const int part = threadIdx.x & 7;
 
     if (static_cast<int>(blockIdx.y) >= a.copy.pool.kv_heads) {
-        const int head0 = (blockIdx.y - a.copy.pool.kv_heads) * kQueryHeads, heads = min(kQueryHeads, a.q_heads - head0);
-        const int rows = to - from, bits = rows <= 1 ? 0 : 32 - __builtin_clz(rows - 1);       // (a power of two of them side by side)
-        const int slot = threadIdx.x >> 3, t = from + (slot & ((1 << bits) - 1)), step = kTileTokens >> bits;
-        if (t >= to) return;
+        const int of = blockIdx.y - a.copy.pool.kv_heads, lane = threadIdx.x & 63;
+        const int t = of % (kTileTokens / kQueryRows) * kQueryRows + (threadIdx.x >> 6), head0 = of / (kTileTokens / kQueryRows) * query_heads_of(D) + lane / kLanes;
+        if (t < from || t >= to) return;
         const int64_t row = u.seq.start + (t - first);
-        const Rotation<D, INTERLEAVED> rotation(a, a.q_weight, part, true, row, tile_token + t);
-        for (int h = slot >> bits; h < heads; h += step) {
-            half8_t x[kRuns], partner[kRuns];
-            rotation.load(a.q.data + row * a.q.row + (head0 + h) * a.q.head, x, partner);
-            rotation.apply(x, partner);
-            uint16_t* y = a.q_out.data + row * a.q_out.row + (head0 + h) * a.q_out.head;
+        const Turn<D, INTERLEAVED> turn(a, lane % kLanes, true, row, tile_token + t);
+        const uint16_t* q = a.q.data + row * a.q.row;
+        typename Turn<D, INTERLEAVED>::Runs x[kQuerySets] = {};
 #pragma unroll
-            for (int r = 0; r < kRuns; ++r) *reinterpret_cast<half8_t*>(y + 8 * (part * kRuns + r)) = x[r];
+        for (int i = 0; i < kQuerySets; ++i)
+            if (head0 + i * (64 / kLanes) < a.q_heads) x[i] = turn.load(q + (head0 + i * (64 / kLanes)) * a.q.head);
+#pragma unroll
+        for (int i = 0; i < kQuerySets; ++i) {
+            const int head = head0 + i * (64 / kLanes);
+            const auto y = turn.apply(x[i], a.q_weight, a.eps);
+            if (head < a.q_heads) turn.store(a.q_out.data + row * a.q_out.row + head * a.q_out.head, y);
         }
         return;
     }
 
-    const int t = threadIdx.x >> 3;
+    const int t = threadIdx.x >> 3, part = threadIdx.x & 7;
     const bool fresh = t >= from && t < to;
     Codes<D> codes{};
     if (fresh) {
         const int64_t row = u.seq.start + (t - first);
-        const Rotation<D, INTERLEAVED> rotation(a, a.k_weight, part, true, row, tile_token + t);
-        half8_t x[kRuns], partner[kRuns], y[kRuns];
-        rotation.load(a.copy.k.data + row * a.copy.k.row + u.head * a.copy.k.head, x, partner);
         const uint16_t* v_at = a.copy.v.data + row * a.copy.v.row + u.head * a.copy.v.head + part * kOwn;
+        half8_t x[kRuns], y[kRuns];
 #pragma unroll
         for (int r = 0; r < kRuns; ++r) y[r] = reinterpret_cast<const half8_t*>(v_at)[r];
-        rotation.apply(x, partner);
-        if (a.k_out.data) {
-            uint16_t* out = a.k_out.data + row * a.k_out.row + u.head * a.k_out.head + part * kOwn;
-#pragma unroll
-            for (int r = 0; r < kRuns; ++r) reinterpret_cast<half8_t*>(out)[r] = x[r];
+        if (part < kLanes) {        // (with heads of 64 half of the threads)
+            const Turn<D, INTERLEAVED> turn(a, part, true, row, tile_token + t);
+            const auto key = turn.apply(turn.load(a.copy.k.data + row * a.copy.k.row + u.head * a.copy.k.head), a.k_weight, a.eps);
+            if (a.k_out.data) turn.store(a.k_out.data + row * a.k_out.row + u.head * a.k_out.head, key);
+            turn.store(keys[t], key);
         }
-        const Quantised<kOwn> k = quantise<kOwn>(x), v = quantise<kOwn>(y);
+        // (a token's threads are of one wavefront, whose operations LDS takes in order)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) codes.k_words[i / 8] |= k.code[i] << nibble(i % 8), codes.v_bytes[i / 4] |= v.code[i] << 8 * (i % 4);
+        for (int r = 0; r < kRuns; ++r) x[r] = *reinterpret_cast<const half8_t*>(&keys[t][part * kOwn + 8 * r]);
+        const Quantised<kOwn> k = quantise<kOwn>(x);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) codes.k_words[i / 8] |= k.code[i] << nibble(i % 8);
         codes.k_parameters = __builtin_bit_cast(uint32_t, half2_t{k.low, k.step});
+        const Quantised<kOwn> v = quantise<kOwn>(y);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) codes.v_bytes[i / 4] |= v.code[i] << 8 * (i % 4);
         codes.v_step = __builtin_bit_cast(uint16_t, v.step), codes.v_low = __builtin_bit_cast(uint16_t, v.low);
     }
     if (u.page < 0 || to <= from) return;
@@ -362,7 +347,7 @@ gqsa_status_t cache_append_rotated(gqsa_cache* c, const RotateCall& call, const 
     const RotatedArgs a{{pool_of(c), call.k, v, seqs}, call.q, call.q_out, call.k_out, call.q_weight, call.k_weight, call.table, call.positions,
                         call.n_positions, call.q_heads, call.rotary_dim / 16, call.eps};
     dim3 grid = copy_grid(c, seqs);
-    grid.y += (call.q_heads + kQueryHeads - 1) / kQueryHeads;
+    grid.y += kTileTokens / kQueryRows * ((call.q_heads + query_heads_of(c->head_dim) - 1) / query_heads_of(c->head_dim));
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (c->head_dim == 128) launch_append<128>(a, call.interleaved != 0, grid, s);
     else launch_append<64>(a, call.interleaved != 0, grid, s);
