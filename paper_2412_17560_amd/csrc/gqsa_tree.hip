@@ -123,8 +123,8 @@ struct RawHalf {
     }
 };
 
-// What an edge asks for, where some rows do not see some of the tile's tokens, or it has `left` tokens only: those behind stand for zero, and values that are NaN
-// stand for zero too, but are noted.
+// What an edge asks for, where some rows do not see some of the tile's tokens, or it has `left` tokens only (an absent one none): those behind stand for zero, and values
+// that are NaN stand for zero too, but are noted.
 template <int D>
 __device__ __forceinline__ void trim_keys(RawHalf<D>& raw, int half, int lane, int left)
 {
@@ -306,12 +306,12 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
         const auto fetch_keys = [&] {
             asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
             raw.fetch_keys(places);
-            if (next_first + kTileTokens > before) trim_keys<D>(raw, my_half, opaque(lane), left_of(next_first));
+            if (next_first < 0 || next_first + kTileTokens > before) trim_keys<D>(raw, my_half, opaque(lane), left_of(next_first));
         };
         const auto fetch_values = [&](int buffer) {
             asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
             raw.fetch_values(places);
-            if (next_first + kTileTokens > before) trim_values<D>(raw, my_half, opaque(lane), left_of(next_first), shared.nan_of[buffer][my_tile]);
+            if (next_first < 0 || next_first + kTileTokens > before) trim_values<D>(raw, my_half, opaque(lane), left_of(next_first), shared.nan_of[buffer][my_tile]);
             if (my_half == 0 && opaque(lane) == 0) shared.first[buffer][my_tile] = next_first;
         };
         constexpr int kStages = 2 * (D / 32);

@@ -29,6 +29,7 @@ struct VerifyShared {
     float probability[kMostRows], drawn_from[kMostRows], uniform[kMostRows];
     uint32_t taken[kVerifyChunk / 32];      // of the chunk's tokens, those of children
     double upto[kMostRuns];                 // running sums of the runs
+    uint64_t positive[kMostRuns / 64];      // runs whose own sum is
     double part[kWaves];
     int row, depth, n_children, last, run, found, last_positive;
 };
@@ -259,8 +260,11 @@ __global__ __launch_bounds__(kThreads, 2) void verify_kernel(VerifyCall c, int c
         if (wave == 0) {
             double before = 0.0;
             for (int i0 = 0; i0 < runs; i0 += 64) {
-                const double upto = before + running_sum(i0 + lane < runs ? shared.upto[min(i0 + lane, runs - 1)] : 0.0);
+                const double own = i0 + lane < runs ? shared.upto[min(i0 + lane, runs - 1)] : 0.0, upto = before + running_sum(own);
                 if (i0 + lane < runs) shared.upto[i0 + lane] = upto;
+                // (two running sums with nothing between them may differ in their last bits, as each lane adds in an order of its own)
+                const uint64_t positive = __builtin_amdgcn_ballot_w64(own > 0.0);
+                if (lane == 0) shared.positive[i0 / 64] = positive;
                 before = lane_of(upto, 63);
             }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -269,12 +273,10 @@ __global__ __launch_bounds__(kThreads, 2) void verify_kernel(VerifyCall c, int c
             const double border = static_cast<double>(final) * before;
             int at = -1, last = 0;
             for (int i0 = 0; i0 < runs && at < 0; i0 += 64) {
-                const int i = min(i0 + lane, runs - 1);
-                const double upto = shared.upto[i];
-                const uint64_t beyond = __builtin_amdgcn_ballot_w64(i0 + lane < runs && upto > border);
-                const uint64_t grows = __builtin_amdgcn_ballot_w64(i0 + lane < runs && upto > (i > 0 ? shared.upto[i - 1] : 0.0));
+                const uint64_t positive = shared.positive[i0 / 64];
+                const uint64_t beyond = __builtin_amdgcn_ballot_w64(shared.upto[min(i0 + lane, runs - 1)] > border) & positive;
                 if (beyond) at = i0 + __builtin_ctzll(beyond);
-                if (grows) last = i0 + 63 - __builtin_clzll(grows);
+                if (positive) last = i0 + 63 - __builtin_clzll(positive);
             }
             if (lane == 0) shared.run = at < 0 ? last : at, shared.found = 1 << 30, shared.last_positive = -1;
         }

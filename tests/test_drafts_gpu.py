@@ -313,6 +313,27 @@ def test_what_a_row_does_not_see_does_not_matter(n, room):
 
 
 @roomy
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("length, absent", [(70, []), (200, []), (200, [1]), (300, [0, 4]), (129, [3])])
+def test_tiles_that_are_not_there(length, absent, dim, room):
+    """Behind the last tile of a step, and where a sequence has no page: nothing of what lies in the cache's other pages, all of them NaN, gets into a result."""
+    n, page = 40, 32
+    c = Cached([0], 2, dim, page, seed=length, room=length + n, spare=3)
+    (unused, *_) = sorted(set(range(c.n_pages)) - set(c.pages[0]) - {0})
+    c.pages[c.pages == 0] = unused                          # page 0 belongs to nobody
+    wild = np.full((c.n_pages * page, 2, dim), np.nan, np.float16)
+    everything = np.arange(c.n_pages, dtype=np.int32)[None]
+    gq.gqsa_cache_append(c.cache, dev(wild), dev(wild), dev(everything), ints(len(wild)), ints(0, len(wild)))
+    c.append([c.some(length + n)], [c.some(length + n)])
+    c.pages[0, absent] = -1
+    sees = drafts.ancestors(random_tree(c.rng, n, 4))
+    q, out = _attend_tree(c, [sees], 8, room=room)
+    there = ~np.isin(np.arange(length + n) // page, absent)
+    c.k, c.v = ([x[0][there]] for x in (c.k, c.v))
+    _check_tree(c, q, out, [sees])
+
+
+@roomy
 @pytest.mark.parametrize("n", [2, 50])
 def test_infinite_queries_of_a_tree(n, room):
     c = Cached([90], 1, 64, 32, seed=16)
@@ -582,6 +603,23 @@ def test_verify_every_border(drawn):
                  (p[:1], np.zeros(1, np.int32), np.zeros(1, np.float32), None, None) for _ in range(n)]
     verifier = gq.gqsa_verify_create(n, vocab)
     _check_verified(sequences, finals, _verify(verifier, sequences, finals, pad=1))
+
+
+@pytest.mark.parametrize("vocab, most", [(128256, 60000), (200000, 3000), (40000, 39000)])
+def test_verify_a_last_number_of_one_draws_the_last_token_with_a_weight(vocab, most):
+    """No running sum passes the whole sum, and tokens behind the last positive weight are not drawn however sums are rounded; nor those between two weights."""
+    rng, sequences, last = np.random.default_rng(vocab), [], []
+    for i in range(64):
+        p = np.zeros((1, vocab), np.float32)
+        at = rng.integers(1, most)
+        p[0, :at] = rng.random(at, dtype=np.float32) ** 4 * (rng.random(at) < [1.0, 0.001][i % 2])
+        p[0, 0] = 0.25
+        p /= p.sum()
+        sequences.append((p, np.zeros(1, np.int32), np.zeros(1, np.float32), None, None))
+        last.append(int(np.flatnonzero(p[0] > 0)[-1]))
+    verifier = gq.gqsa_verify_create(64, vocab)
+    for final in (1.0, 2.0):
+        assert list(_verify(verifier, sequences, [final] * 64)[1]) == last
 
 
 def test_verify_siblings_with_the_same_token_and_tokens_and_parents_outside():
