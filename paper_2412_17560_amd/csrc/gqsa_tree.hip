@@ -1,13 +1,22 @@
 // Attention of a tree's rows over the 4-bit cache where a head of the cache has many rows (gqsa_cache_attend_tree; with few of them, the kernel of gqsa_cache_attend has it).
+//   s_j = scale q k_j for the tokens j before the rows and those of the rows that the mask names;   m = max s_j,   out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m)
+// in one pass over the tokens: maximum (as a reference that follows it from 2^7 below, see gqsa_cache.hip), sum and weighted sum go along in fp32, weights are rounded to
+// fp16 as the second product takes them, and their sum is of the rounded ones, so that the rounding of the largest weight cancels.
 //
 // What the kernel for few rows spends its time on is turning codes into numbers, anew for every 16 rows.  Here a workgroup of 8 wavefronts takes 128 rows of a
 // head of the cache (or 64), and 128 tokens at a time: every wavefront turns half a tile of 32 tokens into fp16 numbers in LDS, one step ahead of the products, and
 // then takes 32 rows with every second (fourth) part of the step's tokens.  Both products are 32x32x16 ones, S^T = K Q^T and O^T = V^T P^T: a lane holds scores
 // of one row only, and holds them as the second product wants its operand, if keys go into the first one in the order in which a word of value codes has its tokens.
+//
+// Bound: 16 sequences of 4160 tokens, 64 rows of 32 heads over 8 (69 GFLOP, 52 us at the rate of a large fp16 product): 94 us, of which the join is 7 and start and end some 12;
+// within the steps of some 4800 cycles the vector units are busy for 43 % of the cycles (softmax, numbers of codes), the matrix cores for 32 %, LDS for 32 %.  One sequence of
+// 131072 tokens, 16 rows of 64 heads over 8 (69 GFLOP): 100 us.  The kernel for few rows takes 202 and 166 for these.
+// Not kept: halves of the workgroup out of phase, one at products and one at numbers, with two barriers a step (no faster, and registers in memory); 32 rows a workgroup without sharing
+// through LDS (16 x 1000 tokens with 128 rows of 8 heads 29 us instead of 37, 16 x 4160 with 256 131 instead of 94); priorities around the second product (no change); joining within
+// the launch by the workgroup that ends last (31 to 50 us on top, for the 4 to 7 of the second launch).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <climits>
 #include <cmath>
 
 #include "gqsa_cache_attend.hpp"
@@ -51,7 +60,6 @@ struct alignas(1024) TreeShared {
 template <int D>
 __device__ __forceinline__ int key_at(int token, int run) { return token * D + 8 * (run ^ (D == 128 ? token & 15 : (token >> 1) & 7)); }
 __device__ __forceinline__ int value_at(int element, int quad) { return element * 32 + 8 * (quad ^ (element >> 2 & 3)); }
-
 
 __device__ __forceinline__ uint32_t lds_address(const void* p)
 {
@@ -208,7 +216,7 @@ __device__ __forceinline__ int tree_steps(const Sequence& q)
     return max(static_cast<int>(static_cast<unsigned>(q.length + kStepTiles * kTileTokens - 1) / static_cast<unsigned>(kStepTiles * kTileTokens)), 1);
 }
 
-// As in the attention of few rows, all steps of all sequences, heads and blocks of rows are dealt evenly to the workgroups.  Where a block lies in several of them each leaves its
+// As in the attention of few rows, all steps of all sequences, heads and blocks of rows are dealt evenly to the workgroups, one to a CU (LDS holds no more).  Where a block lies in several of them each leaves its
 // maximum, sum and weighted sum of every row in the workspace, and a second launch joins them.  GROUPS: wavefronts with rows of their own.
 template <int D, int GROUPS>
 __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
