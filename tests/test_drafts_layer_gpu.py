@@ -116,6 +116,79 @@ def test_steps_one_after_the_other(dim, heads, kv_heads, page, cached, counts, r
     assert moved > 0
 
 
+@pytest.mark.parametrize("room", [0, 70000])                  # the attention for few rows, and for many
+def test_offsets_that_pass_32_bits(room):
+    """Pages behind the fourth gigabyte of a cache, rows of queries, results and probabilities 2^28 elements apart."""
+    heads, kv_heads, dim, rows, vocab = 64, 1, 128, 9, 3000
+    c = Cached([600], kv_heads, dim, 256, seed=12)
+    big = gq.gqsa_cache_create(5 * 2 ** 30 // (256 * 160 * kv_heads) + 1, 256, kv_heads, dim)
+    n = gq.gqsa_cache_info(big)["n_pages"]
+    k, v = c.k[0], c.v[0]
+    c.cache, c.n_pages, c.k, c.v = big, n, [k[:0]], [v[:0]]
+    c.pages = np.array([[n - 1, 0, n - 2]], np.int32)
+    c.append([k], [v])
+    wide = np.pad(c.pages, [(0, 0), (0, max(0, room // 256 - 3))], constant_values=-1)
+    parents = np.array([-1, 0, 0, 1, 2, 2, 4, 6, 7], np.int32)
+    sees = drafts.ancestors(parents)
+    table, positions = _table(700, dim // 2), (600 + sees.sum(axis=1) - 1).astype(np.int32)
+    apart = torch.empty((rows, 1 << 28), dtype=torch.float16, device="cuda")
+    q, out = (apart[:, at:at + heads * dim].view(rows, heads, dim) for at in (0, 1 << 20))
+    x, new_k, new_v = normal(c.rng, rows, heads, dim), c.some(rows), c.some(rows)
+    q.copy_(dev(x))
+    lengths, starts = ints(600 + rows), ints(0, rows)
+    gq.gqsa_cache_append_rotated(big, q, dev(new_k), dev(new_v), dev(positions), dev(table), dev(c.pages), lengths, starts, q_out=q)
+    want = drafts.norm_rotate_rounded(x, positions, table)
+    assert np.array_equal(q.cpu().numpy(), want)
+    gq.gqsa_cache_attend_tree(big, q, dev(wide), lengths, starts, dev(drafts.mask_words(sees, 1)), out=out)
+    k, v = np.concatenate([k, drafts.norm_rotate_rounded(new_k, positions, table)]), np.concatenate([v, new_v])
+    attended, size = drafts.tree_attention(want, ref.cache_values(k), ref.cache_values(v), dim ** -0.5, sees)
+    assert (np.abs(out.cpu().numpy() - attended) <= 2e-3 * size + 1e-4).all()
+    del q, out, apart
+    target = c.rng.random((rows, vocab)).astype(np.float32)
+    tokens, uniforms = c.rng.integers(0, vocab, rows).astype(np.int32), np.zeros(rows, np.float32)
+    target /= target.sum(axis=1, keepdims=True)
+    uniforms[1] = 1.0                                       # the way goes by row 2 and 4 to the last row
+    spread = torch.empty((rows, 1 << 28), dtype=torch.float32, device="cuda")[:, :vocab]
+    spread.copy_(dev(target))
+    path, drawn, accepted = gq.gqsa_verify(gq.gqsa_verify_create(1, vocab), spread, dev(tokens), dev(uniforms), dev(np.array([0.7], np.float32)), starts, parents=dev(parents))
+    way, last = drafts.verify(target, tokens, uniforms, np.float32(0.7), parents)
+    assert way == [0, 2, 4, 6, 7, 8] and path.tolist() == way + [-1] * 3 and drawn.tolist()[5] == last and accepted.tolist() == [5]
+    gq.gqsa_cache_keep(big, dev(c.pages), lengths, starts, path, accepted)
+    of = list(range(600)) + [600 + i for i in way]
+    c.k, c.v = [k[of]], [v[of]]
+    c.check()
+    gq.gqsa_cache_free(big)
+
+
+def test_a_step_on_another_stream_makes_its_arrays_there():
+    """All four calls with a stream of their own, also as its number, and with results that the calls allocate."""
+    c, d = (Cached([45], 2, 64, 32, seed=2, room=40) for _ in range(2))
+    rng, parents, vocab = np.random.default_rng(5), np.array([-1, 0, 0, 2], np.int32), 500
+    sees = drafts.ancestors(parents)
+    q, k, v = normal(rng, 4, 4, 64), normal(rng, 4, 2, 64), normal(rng, 4, 2, 64)
+    target = rng.random((4, vocab)).astype(np.float32)
+    tokens, uniforms, finals = rng.integers(0, vocab, 4).astype(np.int32), np.array([0, 1, 0, 0], np.float32), np.array([0.5], np.float32)
+    fixed = [dev(a) for a in (q, k, v, drafts.mask_words(sees, 1), target, tokens, uniforms, finals, parents)]
+    lengths, starts = ints(49), ints(0, 4)
+    other = torch.cuda.Stream()
+    results = []
+    for x, stream in ((c, None), (d, other), (c, other.cuda_stream)):
+        if stream is not None:
+            other.wait_stream(torch.cuda.current_stream())
+        pages, verifier = dev(x.pages), gq.gqsa_verify_create(1, vocab)
+        torch.cuda.synchronize()
+        turned, _ = gq.gqsa_cache_append_rotated(x.cache, *fixed[:3], None, dev(_table(64, 32)), pages, lengths, starts, stream=stream)
+        attended = gq.gqsa_cache_attend_tree(x.cache, turned, pages, lengths, starts, fixed[3], stream=stream)
+        path, out, accepted = gq.gqsa_verify(verifier, *fixed[4:8], starts, parents=fixed[8], stream=stream)
+        gq.gqsa_cache_keep(x.cache, pages, lengths, starts, path, accepted, stream=stream)
+        kept = gq.gqsa_cache_read(x.cache, pages, ints(48), ints(0, 48), *(torch.empty((48, 2, 64), dtype=torch.float16, device="cuda") for _ in range(2)), stream=stream)
+        torch.cuda.synchronize()
+        results.append([t.cpu().numpy() for t in (turned, attended, path, out, accepted, *kept)])
+    assert list(results[0][2]) == [0, 2, 3, -1]
+    for other_results in results[1:]:
+        assert all(np.array_equal(a, b) for a, b in zip(results[0], other_results))
+
+
 def test_drafts_of_a_layer_are_its_steps():
     """A chain that is kept whole leaves what as many steps of one token leave, and each row attends to what the step's row attends to."""
     import gqsa_inputs as gi
