@@ -9,8 +9,10 @@
 // of one row only, and holds them as the second product wants its operand, if keys go into the first one in the order in which a word of value codes has its tokens.
 //
 // Bound: 16 sequences of 4160 tokens, 64 rows of 32 heads over 8 (69 GFLOP, 52 us at the rate of a large fp16 product): 94 us, of which the join is 7 and start and end some 12;
-// within the steps of some 4800 cycles the vector units are busy for 43 % of the cycles (softmax, numbers of codes), the matrix cores for 32 %, LDS for 32 %.  One sequence of
+// within the steps of some 4800 cycles the vector units are busy for 43 % of the cycles (softmax, numbers of codes), the matrix cores for 31 %, LDS for 32 %.  Without the products
+// it would be 80, without making numbers 77, with them but without their stores to LDS 79, without exponentials 88, without reading operands 96: the stores, 64 KB a step, stand most in the way.  One sequence of
 // 131072 tokens, 16 rows of 64 heads over 8 (69 GFLOP): 100 us.  The kernel for few rows takes 202 and 166 for these.
+// Weights made between the products that do not need them yet gain 1 %.
 // Not kept: halves of the workgroup out of phase, one at products and one at numbers, with two barriers a step (no faster, and registers in memory); 32 rows a workgroup without sharing
 // through LDS (16 x 1000 tokens with 128 rows of 8 heads 29 us instead of 37, 16 x 4160 with 256 131 instead of 94); priorities around the second product (no change); joining within
 // the launch by the workgroup that ends last (31 to 50 us on top, for the 4 to 7 of the second launch).
@@ -359,6 +361,19 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
 #pragma unroll
             for (int e = 0; e < kAhead; ++e) x[0][e] = value_operand(buffer, e);
         };
+        // The weights of 8 / (D / 32) scores; D / 32 times these are an operand, the next of which is made between the products with the one before.
+        float reference;
+        const auto weigh_more = [&](int n) {
+            constexpr int kOnce = 8 / (D / 32);
+            const int i = n / (D / 32), e0 = n % (D / 32) * kOnce;
+            const half2_t ones = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
+#pragma unroll
+            for (int e = e0; e < e0 + kOnce; ++e)
+                p[i][e] = static_cast<_Float16>(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + e], a.scale_log2, -reference)));
+            // (the sum of the weights as the product has them, rounded: half the additions)
+#pragma unroll
+            for (int e = e0; e < e0 + kOnce; e += 2) sum = __builtin_amdgcn_fdot2(half2_t{p[i][e], p[i][e + 1]}, ones, sum, false);
+        };
         const auto weigh = [&] {
             all_seen = true;
 #pragma unroll
@@ -394,23 +409,20 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d) out[d] *= shrink;
             }
-            const float reference = top == kMinusInf ? 0.0f : top;
+            reference = top == kMinusInf ? 0.0f : top;
 #pragma unroll
-            for (int i = 0; i < 2 * kPieces; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    p[i][e] = static_cast<_Float16>(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + e], a.scale_log2, -reference)));
-            // (the sum of the weights as the product has them, rounded: half the additions)
-            const half2_t ones = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
-#pragma unroll
-            for (int i = 0; i < 2 * kPieces; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) sum = __builtin_amdgcn_fdot2(half2_t{p[i][e], p[i][e + 1]}, ones, sum, false);
+            for (int n = 0; n < D / 32; ++n) weigh_more(n);
         };
         const auto add_values = [&](int buffer) {
-            stream_operands<2 * kPieces * (D / 32), kStages>(x, [&](int n) { return value_operand(buffer, n); },
-                                                             [&](int n, half8_t v) { out[n % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[n / (D / 32)], out[n % (D / 32)], 0, 0, 0); },
-                                                             put_values_of(buffer ^ 1));
+            const auto put = put_values_of(buffer ^ 1);
+            constexpr int kProducts = 2 * kPieces * (D / 32);
+            stream_operands<kProducts, kProducts>(x, [&](int n) { return value_operand(buffer, n); },
+                                                  [&](int n, half8_t v) { out[n % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[n / (D / 32)], out[n % (D / 32)], 0, 0, 0); },
+                                                  [&](int n) {
+                                                      if (n + D / 32 < kProducts) weigh_more(n + D / 32);
+#pragma unroll
+                                                      for (int i = n * kStages / kProducts; i < (n + 1) * kStages / kProducts; ++i) put(i);
+                                                  });
             if (!all_seen) {
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j) {
