@@ -14,7 +14,8 @@
 // 131072 tokens, 16 rows of 64 heads over 8 (69 GFLOP): 100 us.  The kernel for few rows takes 202 and 166 for these.
 // Weights made between the products that do not need them yet gain 1 %.
 // Not kept: halves of the workgroup out of phase, one at products and one at numbers, with two barriers a step (no faster, and registers in memory); 32 rows a workgroup without sharing
-// through LDS (16 x 1000 tokens with 128 rows of 8 heads 29 us instead of 37, 16 x 4160 with 256 131 instead of 94); priorities around the second product (no change); joining within
+// through LDS (16 x 1000 tokens with 128 rows of 8 heads 29 us instead of 37, 16 x 4160 with 256 131 instead of 94); 256 rows a workgroup, so that numbers are made half as often
+// (16 x 4160 with 256 rows 128 us instead of 94, heads of 64 too: half as many blocks are dealt, more of them lie in several workgroups); priorities around the second product (no change); joining within
 // the launch by the workgroup that ends last (31 to 50 us on top, for the 4 to 7 of the second launch).
 #include <hip/hip_runtime.h>
 
@@ -535,7 +536,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
 }
 
 // The parts' results of the blocks that lie in several workgroups, in an order that hangs on the lengths alone.  A workgroup takes 4 rows of a block at a time: D / 4 threads to a row, each
-// with four elements, and the rest of the threads for other parts.
+// with four elements, and the rest of the threads for other parts.  (4 x 8128 tokens, 512 rows of 8 heads, with 256, 512, 1024, 2048, 4096 workgroups 110, 102, 99.5, 99.6, 101 us in all.)
 constexpr int kJoinRows = 4, kJoinThreads = 256, kJoinWorkgroups = 1024;
 
 template <int D, int ROWS>

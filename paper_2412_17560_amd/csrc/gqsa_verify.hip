@@ -5,13 +5,12 @@
 // Its weights are summed in 64 bits: where the drawn token's running sum passes v times the whole is then the same whatever the order of additions
 // (a vocabulary of 128256 has as many borders, and sums in 32 bits would move each of them by 10^-7).
 //
-// A workgroup takes 16384 tokens of a sequence's vocabulary, a wavefront 2048 of them, and finds the way by itself, as this is quicker than to be told.  The sums of the
+// A workgroup takes 16384 tokens of a sequence's vocabulary, a wavefront 2048 of them, and finds the way by itself (to be told would take one more meeting of workgroups).  The sums of the
 // wavefronts' runs go to the workspace, and the last workgroup of a sequence to arrive looks for the token: among the runs first, then among the 2048 of one run.
 //
 // Bound: 64 sequences of 5 rows, 128256 tokens, drawn from a draft: 65.7 MB of target and draft, 10.9 us at the rate of a large read; 17.  Small calls by their waits (rows -> probabilities -> the way ->
-// weights -> arrival -> runs -> weights of one run): 1 sequence of 5 rows and 32000 tokens 8.7, 16 trees of 64 rows 9.4.  Each workgroup finding the way for itself costs fewer than one that
-// tells the others; the way by one wavefront's lanes and ballots, a tree's 64 rows in two ballots a step, took 20.2 to 9.5 us for the trees, and runs of 2048 instead of 512 with sums
-// by lane moves instead of LDS 36.6 to 17.1 for the chains.
+// weights -> arrival -> runs -> weights of one run): 1 sequence of 5 rows and 32000 tokens 8.7, 16 trees of 64 rows 9.4.  A way that one wavefront finds by ballots over
+// 64 rows at a time, runs of 2048 tokens to a wavefront, and sums by lane moves that need no LDS together took the trees from 20.2 to 9.5 us and the chains from 36.6 to 17.1.
 #include <hip/hip_runtime.h>
 
 #include "gqsa_device.hpp"
