@@ -138,19 +138,18 @@ struct Turn {
     bool turns;
     float4_t by[4];             // cosine and sine of the lane's 8 pairs
 
-    __device__ __forceinline__ Turn(const RotatedArgs& a, int p, bool there, int64_t row, int token)
+    __device__ __forceinline__ Turn(const RotatedArgs& a, int p, int64_t row, int token)
     {
         turns = p < a.turned;
         run_a = INTERLEAVED || !turns ? 2 * p : p, run_b = INTERLEAVED || !turns ? 2 * p + 1 : p + a.turned;
-        if (!turns || !there) return;
+        if (!turns) return;
         const int position = a.positions ? a.positions[row] : token;
-        const bool known = position >= 0 && position < a.n_positions;
-        const float4_t* table = reinterpret_cast<const float4_t*>(a.table + (static_cast<int64_t>(known ? position : 0) * a.turned + p) * 16);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            by[i] = table[i];
-            if (!known) by[i] = __builtin_nanf("") + float4_t{};
-        }
+        for (int i = 0; i < 4; ++i) by[i] = __builtin_nanf("") + float4_t{};
+        if (position < 0 || position >= a.n_positions) return;      // (nothing is read for it: a table may have no rows at all)
+        const float4_t* table = reinterpret_cast<const float4_t*>(a.table + (static_cast<int64_t>(position) * a.turned + p) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) by[i] = table[i];
     }
 
     struct Runs {
@@ -225,7 +224,7 @@ __global__ __launch_bounds__(kThreads) void append_rotated_kernel(RotatedArgs a)
         const int t = of % (kTileTokens / kQueryRows) * kQueryRows + (threadIdx.x >> 6), head0 = of / (kTileTokens / kQueryRows) * query_heads_of(D) + lane / kLanes;
         if (t < from || t >= to) return;
         const int64_t row = u.seq.start + (t - first);
-        const Turn<D, INTERLEAVED> turn(a, lane % kLanes, true, row, tile_token + t);
+        const Turn<D, INTERLEAVED> turn(a, lane % kLanes, row, tile_token + t);
         const uint16_t* q = a.q.data + row * a.q.row;
         typename Turn<D, INTERLEAVED>::Runs x[kQuerySets] = {};
 #pragma unroll
@@ -250,7 +249,7 @@ __global__ __launch_bounds__(kThreads) void append_rotated_kernel(RotatedArgs a)
 #pragma unroll
         for (int r = 0; r < kRuns; ++r) y[r] = reinterpret_cast<const half8_t*>(v_at)[r];
         if (part < kLanes) {        // (with heads of 64 half of the threads)
-            const Turn<D, INTERLEAVED> turn(a, part, true, row, tile_token + t);
+            const Turn<D, INTERLEAVED> turn(a, part, row, tile_token + t);
             const auto key = turn.apply(turn.load(a.copy.k.data + row * a.copy.k.row + u.head * a.copy.k.head), a.k_weight, a.eps);
             if (a.k_out.data) turn.store(a.k_out.data + row * a.k_out.row + u.head * a.k_out.head, key);
             turn.store(keys[t], key);

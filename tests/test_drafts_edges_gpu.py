@@ -1,0 +1,44 @@
+"""Where a decoding step of several drafted tokens could go wrong at the edge of what its calls take: against the definitions in float64, on the GPU."""
+from __future__ import annotations
+
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import paper_2412_17560_amd as gq
+from oracle import drafts
+from paper_2412_17560_amd import binding
+from test_attention_gpu import Cached, dev, ints, normal
+from test_drafts_gpu import same, starts_of
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+# ----------------------------------------------------------------------------- a rotation's table without rows
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim, rotary, given", [(64, 32, True), (128, 128, False), (128, 48, True)])
+def test_a_table_without_rows(dim, rotary, given, interleaved):
+    """No position is in it: what would be rotated is NaN, the rest is normed as ever, and nothing is read of it.  (Through the C call: torch has no address for an
+    empty array.  The table begins where an array ends.)"""
+    c = Cached([30, 3], 2, dim, 32, seed=dim + rotary, room=10)
+    counts, lengths = [5, 1], [35, 4]
+    n, starts = sum(counts), starts_of(counts)
+    q, k, v, weight = normal(c.rng, n, 3, dim), c.some(n), c.some(n), normal(c.rng, dim)
+    held = torch.ones(16 * rotary, device="cuda")
+    dq, dk, dv, dw, pages, at, positions = (dev(x) for x in (q, k, v, weight, c.pages, starts, np.arange(-1, n - 1, dtype=np.int32)))
+    q_out, k_out, total = torch.zeros_like(dq), torch.zeros_like(dk), ints(*lengths)
+    p = [C.c_void_p(t.data_ptr()) for t in (dq, dk, dv, dw, positions, q_out, k_out, pages, total, at)]
+    status = binding._lib().gqsa_cache_append_rotated(
+        c.cache.ptr, p[0], 3 * dim, dim, 3, p[1], 2 * dim, dim, p[2], 2 * dim, dim, n, p[3], p[3], 1e-5, C.c_void_p(held.data_ptr() + held.numel() * 4), 0, rotary,
+        interleaved, p[4] if given else None, p[5], 3 * dim, dim, p[6], 2 * dim, dim, p[7], c.pages.shape[1], p[8], p[9], 2, C.c_void_p(torch.cuda.current_stream().cuda_stream))
+    assert status == 0
+    want = []
+    for x in (q, k):
+        y = drafts.norm_rotate_rounded(x, weight=weight, eps=1e-5)
+        y[..., :rotary] = np.nan
+        want.append(y)
+    assert same(q_out.cpu().numpy(), want[0]) and same(k_out.cpu().numpy(), want[1])
+    c.k, c.v = ([np.concatenate([a, new[s:e]]) for a, s, e in zip(held, starts, starts[1:])] for held, new in ((c.k, want[1]), (c.v, v)))
+    c.check()
