@@ -50,6 +50,7 @@ void gqsa_verify_free(gqsa_verifier_t v);
  *   out      [device] int32 [n_rows]: the tokens that stand and the one drawn behind them, from the sequence's first row on, -1 behind.  (-1, too, for a token
  *            drawn where all weights and target[g] are 0)
  *   accepted [device] int32 [n_seqs]: rows on the way behind row 0; -1 for a sequence without rows
+ * A call without rows reads no array and writes `accepted` only; without sequences either (n_seqs 0) it does nothing.
  * Rows that belong to no sequence are left as they are.  n_seqs and vocab as the handle was made for (GQSA_ERR_BUFSIZE).  Results are bit-identical from run to run.  Can be captured.
  */
 gqsa_status_t gqsa_verify(gqsa_verifier_t v, const float* target, int64_t target_row, const float* draft, int64_t draft_row, int vocab, int64_t n_rows,

@@ -47,9 +47,18 @@ gqsa_status_t gqsa_verify(gqsa_verifier_t v, const float* target, int64_t target
                           int32_t* path, int32_t* out, int32_t* accepted, void* hip_stream)
 {
     if (!v) return GQSA_ERR_NULL;
+    if (n_rows == 0) {      // (nothing but `accepted`, whatever the rest is)
+        if (n_seqs < 0) return GQSA_ERR_SHAPE;
+        if (n_seqs == 0) return GQSA_OK;
+        if (!accepted) return GQSA_ERR_NULL;
+        if (!words(accepted)) return GQSA_ERR_ALIGN;
+        if (n_seqs > v->max_seqs) return GQSA_ERR_BUFSIZE;
+        gqsa::VerifyCall c{};
+        c.accepted = accepted, c.vocab = 1, c.n_seqs = n_seqs;
+        return gqsa::verify(v, c, hip_stream);
+    }
     if (n_rows < 0 || n_rows > kMostRows || n_seqs < 1 || vocab < 1) return GQSA_ERR_SHAPE;
-    if (!finals || !accepted) return GQSA_ERR_NULL;
-    if (n_rows > 0 && (!target || !tokens || !uniforms || !path || !out)) return GQSA_ERR_NULL;
+    if (!finals || !accepted || !target || !tokens || !uniforms || !path || !out) return GQSA_ERR_NULL;
     if (target_row < 0 || draft_row < 0 || target_row > (int64_t{1} << 31) || draft_row > (int64_t{1} << 31)) return GQSA_ERR_SHAPE;
     if (!row_starts && n_rows != n_seqs) return GQSA_ERR_SHAPE;
     if (draft && parents) return GQSA_ERR_UNSUPPORTED;

@@ -42,3 +42,35 @@ def test_a_table_without_rows(dim, rotary, given, interleaved):
     assert same(q_out.cpu().numpy(), want[0]) and same(k_out.cpu().numpy(), want[1])
     c.k, c.v = ([np.concatenate([a, new[s:e]]) for a, s, e in zip(held, starts, starts[1:])] for held, new in ((c.k, want[1]), (c.v, v)))
     c.check()
+
+
+# ----------------------------------------------------------------------------- calls without rows
+@pytest.mark.parametrize("n_seqs", [0, 1, 3])
+@pytest.mark.parametrize("drawn", [False, True])
+def test_verify_without_rows(n_seqs, drawn):
+    verifier = gq.gqsa_verify_create(3, 40000)
+    target = torch.empty((0, 40000), device="cuda")
+    finals, accepted = torch.zeros(n_seqs, device="cuda"), torch.full((n_seqs,), 7, dtype=torch.int32, device="cuda")
+    for starts in (ints(*[0] * (n_seqs + 1)), None):
+        path, out, got = gq.gqsa_verify(verifier, target, ints(), torch.empty(0, device="cuda"), finals, starts, parents=None if drawn else ints(),
+                                        draft=target if drawn else None, accepted=accepted.clone())
+        assert path.shape == out.shape == (0,) and got.tolist() == [-1] * n_seqs
+
+
+@pytest.mark.parametrize("n_seqs", [0, 2])
+def test_a_layers_drafted_step_without_rows(n_seqs):
+    """Nothing is appended, attended, verified or kept, and the cache is what it was."""
+    import gqsa_inputs as gi
+    from paper_2412_17560_amd.attention_layer import AttentionLayer, rotary_table
+
+    hidden, heads, kv_heads, dim = 256, 4, 2, 64
+    sizes = [(heads * dim, hidden), (kv_heads * dim, hidden), (kv_heads * dim, hidden), (hidden, heads * dim)]
+    c = Cached([40, 3], kv_heads, dim, 32, room=64)
+    layer = AttentionLayer(*[gq.gqsa_pack(gi.dense_weight(n, k, seed=i), 16, 4, 0.5) for i, (n, k) in enumerate(sizes)], heads, rotary_table(64, dim), c.cache)
+    pages, lengths, starts = dev(c.pages[:n_seqs]), ints(*[40, 3][:n_seqs]), ints(*[0] * (n_seqs + 1))
+    x = torch.empty((0, hidden), dtype=torch.float16, device="cuda")
+    assert layer.drafts(x, ints(), pages, lengths, starts, torch.empty((0, 1), dtype=torch.int32, device="cuda")).shape == (0, hidden)
+    path, _, accepted = gq.gqsa_verify(gq.gqsa_verify_create(2, 50), torch.empty((0, 50), device="cuda"), ints(), torch.empty(0, device="cuda"),
+                                       torch.zeros(n_seqs, device="cuda"), starts, parents=ints())
+    layer.keep(pages, lengths, starts, path, accepted)
+    c.check()
