@@ -17,7 +17,7 @@
  *
  * Several sequences lie one behind the other in the rows: sequence b has the rows row_starts[b] .. row_starts[b + 1] - 1
  * (row_starts [device] int32[n_seqs + 1], or NULL: one row per sequence).  Values on the device cannot be refused by the host,
- * so the kernels bound them: rows outside the given array are not touched, a length counts as at least 0 and, in attention, at most
+ * so the kernels bound them: rows outside the given array are not touched, a length counts as at least 0 and, in gqsa_cache_attend, at most
  * what the sequence's pages hold, and a page number outside the cache makes the tokens of that page absent (not read, not written).
  */
 #ifndef GQSA_ATTENTION_H
@@ -149,7 +149,8 @@ gqsa_status_t gqsa_cache_attend(gqsa_cache_t c, const void* q, int64_t q_row_str
  * sees no token is zero.
  *   masks    [device] int32 [n_rows, mask_words]: bit j % 32 of word j / 32 stands for row j of the row's own sequence (bits of rows that it does not have, and rows
  *            from 32 mask_words on: not seen); mask_words 1 .. 2^15 (GQSA_ERR_UNSUPPORTED)
- * Keys and values that a row does not see have no effect on it, whatever they hold.  The rest as in gqsa_cache_attend.
+ * Keys and values that a row does not see have no effect on it, whatever they hold.  Rows that would be tokens beyond what the pages hold, which gqsa_cache_append leaves
+ * out, are seen by nobody, and see what there is like any other.  The rest as in gqsa_cache_attend.
  */
 gqsa_status_t gqsa_cache_attend_tree(gqsa_cache_t c, const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads,
                                      int64_t n_rows, const int32_t* pages, int max_pages, const int32_t* lengths,

@@ -346,9 +346,9 @@ struct alignas(16) AttendShared {
 constexpr int kHeld = 2;             // tiles that a wavefront holds: the one at work, and those under way
 constexpr int kAttendWaves = 4;      // wavefronts of a workgroup; a step: one tile for each
 
-__device__ __forceinline__ int steps_of(const Sequence& q, int step_tiles)
+__device__ __forceinline__ int steps_of(int tokens, int step_tiles)
 {
-    return max(static_cast<int>(static_cast<unsigned>(q.length + step_tiles * kTileTokens - 1) / static_cast<unsigned>(step_tiles * kTileTokens)), 1);
+    return max(static_cast<int>(static_cast<unsigned>(tokens + step_tiles * kTileTokens - 1) / static_cast<unsigned>(step_tiles * kTileTokens)), 1);
 }
 
 // Of 0 / 1 / 2 / 4 / 8 steps a workgroup, us: 143 tokens of 32 heads 7.4 / 6.45 / 6.45 / 6.4 / 6.4; 8 x 3000 tokens, 4 rows, 2 for 14 of 64 11.7 / 11.8 / 9.9 / 10.0 / 10.0;
@@ -380,9 +380,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
     const auto blocks_of = [&](const Sequence& q) { return static_cast<int>((static_cast<unsigned>(q.rows) * per + kRowBlock - 1) / kRowBlock); };
     // A step is one tile for every wavefront; or two, where there are so few that a workgroup has one or two of them: half the parts to join.
     int step_tiles = WAVES;
-    const int most_length = most_tokens(a.seqs, a.pool.page_shift);
+    // (a length beyond the pages is cut; with TREE rows are counted from a sequence's true end all the same)
+    const int room = most_tokens(a.seqs, a.pool.page_shift), most_length = TREE ? INT_MAX : room;
+    const auto tokens_of = [&](const Sequence& q) { return TREE ? min(q.length, room) : q.length; };
     auto deal = deal_out<Sequence>(a.seqs.n_seqs, lane, [&](int b) { return sequence(a.seqs, most_length, b); }, [&](const Sequence& q) {
-        return static_cast<unsigned>(min(static_cast<int64_t>(blocks_of(q)) * steps_of(q, step_tiles) * a.pool.kv_heads, int64_t{INT_MAX}));
+        return static_cast<unsigned>(min(static_cast<int64_t>(blocks_of(q)) * steps_of(tokens_of(q), step_tiles) * a.pool.kv_heads, int64_t{INT_MAX}));
     });
     if (deal.total <= kFewSteps * gridDim.x) {
         step_tiles = 2 * WAVES;
@@ -401,7 +403,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
     int b, within;
     Sequence seq = deal.locate(at, &b, &within);
     while (at < end) {
-        const int blocks = blocks_of(seq), steps = steps_of(seq, step_tiles);
+        const int blocks = blocks_of(seq), steps = steps_of(tokens_of(seq), step_tiles);
         if (within >= blocks * steps * a.pool.kv_heads) {       // (on to the next sequence that has rows)
             within = 0;
             seq = sequence(a.seqs, most_length, ++b);
@@ -413,7 +415,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
         const unsigned row0 = (segment - head * blocks) * kRowBlock;        // of the sequence's rows times the heads of a group
         const int rows = min(static_cast<unsigned>(kRowBlock), seq.rows * per - row0);
         const unsigned token0 = row0 / per, head0 = row0 - token0 * per;    // row r of the block: head (head0 + r) % per of the group, token further on
-        const int before = seq.length - seq.rows;
+        const int before = seq.length - seq.rows, tokens = tokens_of(seq);
 
         // this lane's row
         const bool is_row = (lane & 15) < rows;
@@ -431,7 +433,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
             q[g] += q[g] - q[g];
         }
         // tokens that the block's first and last row see; of a tree, the tokens before the rows and all
-        const int least = TREE ? before : before + token0 + 1, most = TREE ? seq.length : before + token0 + (head0 + rows - 1) / per + 1;
+        const int least = TREE ? before : before + token0 + 1, most = TREE ? tokens : before + token0 + (head0 + rows - 1) / per + 1;
         const int tiles = uniform(min((max(most, 0) + kTileTokens - 1) / kTileTokens, to * step_tiles));
 
         RowState<D> state;
@@ -466,11 +468,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_kernel(AttendArgs a)
             if (raw.first_token + kTileTokens > least) {
                 uint32_t seen = 0;
                 if constexpr (TREE) {
-                    if (is_row) seen = seen_of(a.masks + int64_t{seq.start + row} * a.mask_words, a.mask_words, raw.first_token - before, seq.length - raw.first_token);
+                    if (is_row) seen = seen_of(a.masks + int64_t{seq.start + row} * a.mask_words, a.mask_words, raw.first_token - before, tokens - raw.first_token);
                 }
-                attend_tile<D, true, TREE>(raw, shared.stage[wave], q, state, lane, seq.length, limit, seen, a.scale_log2);
+                attend_tile<D, true, TREE>(raw, shared.stage[wave], q, state, lane, tokens, limit, seen, a.scale_log2);
             } else {
-                attend_tile<D, false, TREE>(raw, shared.stage[wave], q, state, lane, seq.length, limit, 0, a.scale_log2);
+                attend_tile<D, false, TREE>(raw, shared.stage[wave], q, state, lane, tokens, limit, 0, a.scale_log2);
             }
         };
         // kHeld - 1 tiles ahead, in registers that are not copied

@@ -214,9 +214,9 @@ __device__ __forceinline__ void stream_operands(half8_t (&x)[2][kAhead], Read re
     }
 }
 
-__device__ __forceinline__ int tree_steps(const Sequence& q)
+__device__ __forceinline__ int tree_steps(int tokens)
 {
-    return max(static_cast<int>(static_cast<unsigned>(q.length + kStepTiles * kTileTokens - 1) / static_cast<unsigned>(kStepTiles * kTileTokens)), 1);
+    return max(static_cast<int>(static_cast<unsigned>(tokens + kStepTiles * kTileTokens - 1) / static_cast<unsigned>(kStepTiles * kTileTokens)), 1);
 }
 
 // As in the attention of few rows, all steps of all sequences, heads and blocks of rows are dealt evenly to the workgroups, one to a CU (LDS holds no more).  Where a block lies in several of them each leaves its
@@ -232,9 +232,11 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
     const int group = wave % GROUPS, part = wave / GROUPS;
     const unsigned per = a.heads_per_group;
     const auto blocks_of = [&](const Sequence& q) { return static_cast<int>((static_cast<unsigned>(q.rows) * per + kRows - 1) / kRows); };
-    const int most_length = most_tokens(a.seqs, a.pool.page_shift);
-    const auto deal = deal_out<Sequence>(a.seqs.n_seqs, lane, [&](int b) { return sequence(a.seqs, most_length, b); }, [&](const Sequence& q) {
-        return static_cast<unsigned>(min(static_cast<int64_t>(blocks_of(q)) * tree_steps(q) * a.pool.kv_heads, int64_t{INT_MAX}));
+    // (rows are counted from a sequence's true end, also where that lies beyond its pages)
+    const int room = most_tokens(a.seqs, a.pool.page_shift);
+    const auto steps_of = [&](const Sequence& q) { return tree_steps(min(q.length, room)); };
+    const auto deal = deal_out<Sequence>(a.seqs.n_seqs, lane, [&](int b) { return sequence(a.seqs, INT_MAX, b); }, [&](const Sequence& q) {
+        return static_cast<unsigned>(min(static_cast<int64_t>(blocks_of(q)) * steps_of(q) * a.pool.kv_heads, int64_t{INT_MAX}));
     });
     const unsigned total = deal.total, workers = min(gridDim.x, total), me = blockIdx.x;
     if (threadIdx.x == 0) a.splits[me].parts = 0;
@@ -250,10 +252,10 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
     int b, within;
     Sequence seq = deal.locate(at, &b, &within);
     while (at < end) {
-        const int blocks = blocks_of(seq), steps = tree_steps(seq);
+        const int blocks = blocks_of(seq), steps = steps_of(seq);
         if (within >= blocks * steps * a.pool.kv_heads) {       // (on to the next sequence that has rows)
             within = 0;
-            seq = sequence(a.seqs, most_length, ++b);
+            seq = sequence(a.seqs, INT_MAX, ++b);
             continue;
         }
         const int segment = static_cast<unsigned>(within) / static_cast<unsigned>(steps), from = within - segment * steps;
@@ -262,7 +264,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
         const unsigned row0 = (segment - head * blocks) * kRows;        // of the sequence's rows times the heads of a group
         const int rows = min(static_cast<unsigned>(kRows), seq.rows * per - row0);
         const unsigned token0 = row0 / per, head0 = row0 - token0 * per;    // row r of the block: head (head0 + r) % per of the group, token further on
-        const int before = seq.length - seq.rows;
+        const int before = seq.length - seq.rows, tokens = min(seq.length, room);
 
         // this lane's row
         const int own = 32 * group + (lane & 31);
@@ -287,7 +289,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
 
         // The wavefront turns half of every fourth tile into numbers; lane i knows where the i-th of the next 64 lies, so that no load waits for another.
         const int32_t* table = a.seqs.pages + int64_t{b} * a.seqs.max_pages;
-        const int tiles = uniform(min((seq.length + kTileTokens - 1) / kTileTokens, to * kStepTiles));
+        const int tiles = uniform(min((tokens + kTileTokens - 1) / kTileTokens, to * kStepTiles));
         const int my_tile = wave >> 1, my_half = wave & 1, count = to - from;
         const Places<D> places(shared, opaque(lane), wave, kPieces * part, my_tile, my_half);
         // (always the same number of loads: past the end and for absent pages of some tile that is there)
@@ -312,7 +314,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
         };
         const auto load_values = [&] { copy_half(lds_address(shared.raw[wave][1]), after_tile, places.codes + 16 * D, places.parameters + 4 * D); };
         RawHalf<D> raw;
-        const auto left_of = [&](int first_token) { return first_token < 0 ? 0 : seq.length - first_token; };
+        const auto left_of = [&](int first_token) { return first_token < 0 ? 0 : tokens - first_token; };
         // (what has been asked for since may still be under way: two loads)
         const auto fetch_keys = [&] {
             asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
@@ -385,7 +387,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(TreeArgs a)
             // element r of s[j] is row r % 4 + 8 (r / 4) + 4 half of the operand
             if (!all_seen) {
 #pragma unroll
-                for (int j = 0; j < kPieces; ++j) seen[j] = seen_of(mask, a.mask_words, first[j] - before, seq.length - first[j]);
+                for (int j = 0; j < kPieces; ++j) seen[j] = seen_of(mask, a.mask_words, first[j] - before, tokens - first[j]);
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j) {
                     if (!is_row || first[j] < 0) seen[j] = 0;

@@ -7,10 +7,11 @@ import numpy as np
 import pytest
 
 import paper_2412_17560_amd as gq
+from oracle import attention as ref
 from oracle import drafts
 from paper_2412_17560_amd import binding
-from test_attention_gpu import Cached, dev, ints, normal
-from test_drafts_gpu import same, starts_of
+from test_attention_gpu import Cached, _check_attended, dev, ints, normal
+from test_drafts_gpu import random_tree, roomy, same, starts_of
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -74,3 +75,49 @@ def test_a_layers_drafted_step_without_rows(n_seqs):
                                        torch.zeros(n_seqs, device="cuda"), starts, parents=ints())
     layer.keep(pages, lengths, starts, path, accepted)
     c.check()
+
+
+# ----------------------------------------------------------------------------- rows of a tree that pass the end of the pages
+@roomy
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("fit", [12, 7, 1, 0, -3])
+def test_a_trees_rows_beyond_the_pages(dim, fit, room):
+    """The rows that still have a place are the tokens that append has made of them, and see those before them all; the others have none, and see what their masks name of the
+    rest.  The sequence's last two pages are there only, the table's last ones: with room, a table for which the kernel for many rows is taken."""
+    n, heads, kv_heads, page, there = 12, 8, 2, 32, 64
+    wide = -(-65536 * 32 // (n * heads // 16 * page)) if room else 4
+    c = Cached([0], kv_heads, dim, page, seed=fit + dim, room=there)
+    pages = np.full((1, wide), -1, np.int32)
+    pages[0, -2:] = c.pages[0]
+    before = wide * page - fit                                  # tokens before the rows; those that are there are the last 64 of the table's room
+    old = there - max(fit, 0)
+    k, v = c.some(old + n), c.some(old + n)
+    lost = max(-fit, 0)                                         # (of the old ones, appended in a call of their own)
+    for at, end, length in ((0, old, before - lost), (old, old + n, before + n)):
+        gq.gqsa_cache_append(c.cache, dev(k[at:end]), dev(v[at:end]), dev(pages), ints(length), ints(0, end - at))
+    q, sees = normal(c.rng, n, heads, dim), drafts.ancestors(random_tree(c.rng, n, 3))
+    out = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(pages), ints(before + n), ints(0, n), dev(drafts.mask_words(sees, 1))).cpu().numpy()
+    seen = sees.copy()
+    seen[:, max(fit, 0):] = False
+    hk, hv = ref.cache_values(k), ref.cache_values(v)
+    want, size = drafts.tree_attention(q, hk, hv, dim ** -0.5, seen)
+    _check_attended(out, want, size, old + n, hv)
+
+
+@roomy
+def test_lengths_far_beyond_the_pages(room):
+    """Every token that is there lies before the rows, however far."""
+    n, heads, dim, page = 12, 32, 64, 32
+    wide = -(-65536 * 32 // (n * heads // 16 * page)) if room else 2
+    c = Cached([64, 64, 64], 2, dim, page, seed=1)
+    pages = np.full((3, wide), -1, np.int32)
+    pages[:, -2:] = c.pages
+    for b in range(3):
+        gq.gqsa_cache_append(c.cache, dev(c.k[b]), dev(c.v[b]), dev(pages[b:b + 1]), ints(wide * page), ints(0, 64))
+    q, counts = normal(c.rng, n, heads, dim), [5, 4, 3]
+    masks = dev(drafts.mask_words(np.zeros((n, n), bool), 1))
+    out = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(pages), ints(wide * page + 5, 2 ** 31 - 1, 2 ** 31 - 4000), dev(starts_of(counts)), masks).cpu().numpy()
+    for b, (s, e) in enumerate(zip(starts_of(counts), starts_of(counts)[1:])):
+        hk, hv = ref.cache_values(c.k[b]), ref.cache_values(c.v[b])
+        want, size = ref.attention(q[s:e], hk, hv, dim ** -0.5, [64] * (e - s))
+        _check_attended(out[s:e], want, size, 64, hv)
