@@ -10,8 +10,9 @@ import paper_2412_17560_amd as gq
 from oracle import attention as ref
 from oracle import drafts
 from paper_2412_17560_amd import binding
+from test_attention_edges_gpu import SMALL, _check_sum_of_small, _sink
 from test_attention_gpu import Cached, _check_attended, dev, ints, normal
-from test_drafts_gpu import random_tree, roomy, same, starts_of
+from test_drafts_gpu import _check_verified, _verify, probabilities, random_tree, roomy, roomy_pages, same, starts_of
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -121,3 +122,94 @@ def test_lengths_far_beyond_the_pages(room):
         hk, hv = ref.cache_values(c.k[b]), ref.cache_values(c.v[b])
         want, size = ref.attention(q[s:e], hk, hv, dim ** -0.5, [64] * (e - s))
         _check_attended(out[s:e], want, size, 64, hv)
+
+
+# ----------------------------------------------------------------------------- many small weights behind a large one
+@roomy
+@pytest.mark.parametrize("of_sink", [0.0, 1.0])
+@pytest.mark.parametrize("tokens, gap", SMALL)
+def test_many_small_weights_of_a_tree(tokens, gap, of_sink, room):
+    n = 40
+    c = Cached([0], 1, 64, 1024, seed=int(10 * gap), room=tokens)
+    q, k, v = _sink(c.rng, tokens, 1, 1, gap, of_sink, rows=n)
+    c.append([k], [v])
+    pages = roomy_pages(c, n) if room else c.pages
+    masks = drafts.mask_words(np.tri(n, dtype=bool), 2)
+    out = gq.gqsa_cache_attend_tree(c.cache, dev(q), dev(pages), ints(tokens), ints(0, n), dev(masks), scale=1.0).cpu().numpy()
+    hk, hv = ref.cache_values(k), ref.cache_values(v)
+    want, size = ref.attention(q, hk, hv, 1.0, [tokens - n + i + 1 for i in range(n)])
+    _check_sum_of_small(out, want, size, tokens, hv)
+
+
+# ----------------------------------------------------------------------------- many children of one row
+@pytest.mark.parametrize("n, vocab, distinct", [(65, 300, 300), (200, 300, 40), (200, 5000, 5000), (1024, 3000, 700), (1024, 20000, 20000)])
+def test_verify_many_children_of_one_row(n, vocab, distinct):
+    """Stars: more children than the 64 rows that are looked at together, with tokens that come again in the same 64 and in later ones; none stands, one stands alone (with a
+    token that an earlier one has, or has not), any may.  The second half of them has children of its own in a last star."""
+    rng = np.random.default_rng(n + distinct)
+    sequences, finals, ends = [], [], []
+    for case in range(24):
+        target = probabilities(rng, n, vocab)
+        tokens = rng.permutation(vocab)[:distinct][rng.integers(0, distinct, n)].astype(np.int32)
+        if distinct >= n:
+            tokens = rng.permutation(vocab)[:n].astype(np.int32)
+        parents = np.zeros(n, np.int32)
+        parents[0] = -1
+        uniforms = np.ones(n, np.float32)
+        if case % 4 == 1:
+            uniforms[n - 1 - rng.integers(0, n // 3)] = 0.0
+        elif case % 4 == 2:
+            uniforms[1 + rng.integers(0, n - 1)] = 0.0
+        elif case % 4 == 3:
+            uniforms = (0.9 + 0.1 * rng.random(n)).astype(np.float32)
+        if case % 8 >= 4:                                      # (a row in the middle, which stands, has all that come behind it)
+            middle = n // 2 + int(rng.integers(-3, 4))
+            parents[middle + 1:], uniforms[middle] = middle, 0.0
+        sequences.append((target, tokens, uniforms, parents, None))
+        finals.append(rng.random(dtype=np.float32))
+        ends.append(len(drafts.verify(target, tokens, uniforms, finals[-1], parents)[0]))
+    assert {1, 2} <= set(ends)
+    _check_verified(sequences, finals, _verify(gq.gqsa_verify_create(24, vocab), sequences, finals))
+
+
+# ----------------------------------------------------------------------------- the command's steps
+class _Given(torch.Tensor):
+    """Numbers that are what they have been set to."""
+
+    def uniform_(self):
+        return self
+
+
+@pytest.mark.parametrize("count, vocab, cached", [(7, 1024, [40, 3]), (40, 300, [700])])
+def test_replayed_drafted_steps_are_the_eager_ones(count, vocab, cached):
+    """The command's whole step, torch's products and sums in it, from a captured graph: every replay gives what the eager step gives, with eager steps between them."""
+    import gqsa_inputs as gi
+    from paper_2412_17560_amd.attention_layer import AttentionLayer, DraftedSteps, rotary_table
+
+    hidden, heads, kv_heads, dim = 256, 4, 2, 64
+    sizes = [(heads * dim, hidden), (kv_heads * dim, hidden), (kv_heads * dim, hidden), (hidden, heads * dim)]
+    matrices = [gq.gqsa_pack(gi.dense_weight(n, k, seed=i), 16, 4, 0.5) for i, (n, k) in enumerate(sizes)]
+    twins = [Cached(cached, kv_heads, dim, 64, seed=3, room=count + 8 * 7) for _ in range(2)]
+    eager, graphed = (DraftedSteps(AttentionLayer(*matrices, heads, rotary_table(2000, dim), c.cache), dev(c.pages), ints(*cached), count, vocab) for c in twins)
+    for steps in (eager, graphed):
+        steps.uniforms, steps.finals = steps.uniforms.as_subclass(_Given), steps.finals.as_subclass(_Given)
+    rng, graph, kept = np.random.default_rng(count), None, 0
+    for _ in range(7):
+        numbers = rng.random(len(cached) * (count + 1), dtype=np.float32), rng.random(len(cached), dtype=np.float32)
+        for steps in (eager, graphed):
+            steps.uniforms.copy_(dev(numbers[0])), steps.finals.copy_(dev(numbers[1]))
+        want = eager.step()
+        if graph is None:
+            got = graphed.step()                               # (the first call of each kernel loads it)
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                got_by_graph = graphed.step()
+        else:
+            graph.replay()
+            got = got_by_graph
+        torch.cuda.synchronize()
+        assert torch.equal(want, got) and torch.isfinite(got).all()
+        assert all(torch.equal(getattr(eager, name), getattr(graphed, name)) for name in ("before", "last", "generated"))
+        kept = int(eager.generated)
+    assert kept > 7 * len(cached)                              # (drafted tokens stood)
