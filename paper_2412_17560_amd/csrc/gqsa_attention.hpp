@@ -1,5 +1,5 @@
 // Internal definitions of the operators between the q/k/v and the o product (include/gqsa_attention.h): what the C boundary
-// (gqsa_attention_api.cpp) hands to the kernels (gqsa_rotate.hip, gqsa_cache.hip, gqsa_cache_rows.hip, gqsa_prompt.hip).
+// (gqsa_attention_api.cpp) hands to the kernels (gqsa_rotate.hip, gqsa_cache.hip, gqsa_cache_rows.hip, gqsa_tree.hip, gqsa_prompt.hip).
 #pragma once
 
 #include <cstdint>
@@ -36,7 +36,7 @@ struct RotateCall {
     float eps, one_over_dim;
 };
 
-// The tokens of a 4-bit cache are held in tiles of 32 of one head: what 16x16x32 products take (gqsa_cache.hip says in which order).
+// The tokens of a 4-bit cache are held in tiles of 32 of one head: what 16x16x32 products take (gqsa_cache.hpp says in which order).
 constexpr int kTileTokens = 32;
 constexpr int kGroupChannels = 32;      // elements that share low and step
 constexpr int tile_bytes(int head_dim) { return kTileTokens * head_dim + 2 * kTileTokens * (head_dim / kGroupChannels) * 4; }

@@ -1,5 +1,5 @@
 // extern "C" surface of include/gqsa_attention.h: argument checking and the life of a cache handle.  The arithmetic is in
-// gqsa_rotate.hip, gqsa_cache.hip and gqsa_prompt.hip.
+// gqsa_rotate.hip, gqsa_cache.hip, gqsa_cache_rows.hip, gqsa_tree.hip and gqsa_prompt.hip.
 #include <cmath>
 #include <cstdint>
 #include <new>

@@ -1,5 +1,5 @@
 // A paged cache of keys and values in 4 bits (gqsa_cache_append, gqsa_cache_read) and the attention of the newest tokens over it
-// (gqsa_cache_attend).
+// (gqsa_cache_attend; of a tree's rows, gqsa_cache_attend_tree, where they are few: for many, gqsa_tree.hip).
 // (gqsa_cache.hpp says in which order a tile of the cache is held.)
 #include <hip/hip_runtime.h>
 
@@ -216,6 +216,8 @@ __device__ __forceinline__ void hide(typename Raw<D>::words_t& parameters, int l
     }
 }
 
+// One tile for one wavefront.  S^T = K Q^T and O^T = V^T P^T: a lane's scores are then the elements of the operand P^T that the second product wants
+// from it, whatever the tokens' order, as the value codes lie in the same.
 // With TREE a row sees the tile's tokens that `seen` names, else those below `limit`.
 template <int D, bool EDGE, bool TREE>
 __device__ __forceinline__ void attend_tile(const Raw<D>& raw, uint32_t* stage, const half8_t (&q)[D / 32], RowState<D>& state, int lane,
@@ -342,6 +344,114 @@ struct alignas(16) AttendShared {
     float top[WAVES][kRowBlock], sum[WAVES][kRowBlock];
     int last;
 };
+
+// Partial results, which workgroups on other XCDs read: stores and loads at the agent's scope (sc1), past the caches that are not coherent, by offsets
+// in floats.  Nobody has read such a place before in the same launch, and a launch begins with empty caches.
+struct Partials {
+    __amdgpu_buffer_rsrc_t buffer;
+    static constexpr int kAgent = 16;       // sc1
+
+    __device__ __forceinline__ Partials(float* base, int floats) : buffer(__builtin_amdgcn_make_buffer_rsrc(base, 0, floats * 4, 0x00020000)) {}
+    __device__ __forceinline__ void store4(int at, float4_t v) const
+    {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), buffer, at * 4, 0, kAgent);
+    }
+    __device__ __forceinline__ void store2(int at, float a, float b) const
+    {
+        typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)}, buffer, at * 4, 0, kAgent);
+    }
+    __device__ __forceinline__ float4_t load4(int at) const
+    {
+        return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer, at * 4, 0, kAgent));
+    }
+    __device__ __forceinline__ float2 load2(int at) const
+    {
+        typedef float float2_t __attribute__((ext_vector_type(2)));
+        const float2_t v = __builtin_bit_cast(float2_t, __builtin_amdgcn_raw_buffer_load_b64(buffer, at * 4, 0, kAgent));
+        return {v[0], v[1]};
+    }
+};
+
+// (32 / 16 / 8, us: 131072 tokens, 8 heads for 64 45.3 / 42.7 / 42.0; 32768 tokens, 1 for 16 17.8 / 14.5 / 14.5; 4 x 20000 tokens, 4 rows, 8 for 64 40.8 / 41.3 / 44.5)
+constexpr int kFan = 16;        // parts that one workgroup joins alone, unless they are themselves joined ones
+constexpr int kMostParts = (kAttendWorkgroups + kFan - 1) / kFan;       // of which there are up to so many
+static_assert(kMostParts >= kFan, "");
+
+// Joins `parts` (up to kMostParts) partial results of `rows` rows in their order -- place(p): where part p lies -- and hands each four elements of a row to
+// `sink`.  All loads are under way together (or kAhead parts' at a time), or each round of them would cost the latency of memory anew.
+// Called by a whole workgroup; `scratch` is LDS for (2 kMostParts + 1) ROWS floats.
+template <int D, int ROWS, int THREADS, typename Place, typename Sink>
+__device__ __forceinline__ void join(const Partials& partials, int rows, int parts, float* scratch, Place place, Sink sink)
+{
+    constexpr int kSets = (ROWS * (D / 4) + THREADS - 1) / THREADS;      // fours of elements per thread
+    constexpr int kAhead = 32 / kSets < kFan ? 32 / kSets : kFan;
+    float4_t x[kAhead][kSets];
+    const auto load = [&](int p0) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (p0 + j >= parts) break;
+            const int from = place(p0 + j);
+#pragma unroll
+            for (int k = 0; k < kSets; ++k) x[j][k] = partials.load4(from + min(static_cast<int>(threadIdx.x) + k * THREADS, rows * (D / 4) - 1) * 4);
+        }
+    };
+    load(0);
+    float* weights = scratch;               // [part][row]: maximum, then weight
+    float* sums = scratch + kMostParts * ROWS;
+    float* tops = sums + kMostParts * ROWS;      // of all parts
+    for (int i = threadIdx.x; i < parts * rows; i += THREADS) {
+        const int part = i / rows, r = i - part * rows;
+        const float2 top_sum = partials.load2(place(part) + ROWS * D + 2 * r);
+        weights[part * ROWS + r] = top_sum.x, sums[part * ROWS + r] = top_sum.y;
+    }
+    __syncthreads();
+    constexpr int kWeights = (kMostParts * ROWS + THREADS - 1) / THREADS;       // per thread
+    float mine[kWeights];
+#pragma unroll
+    for (int k = 0; k < kWeights; ++k) {
+        const int i = threadIdx.x + k * THREADS;
+        if (i >= parts * rows) break;
+        const int part = i / rows, r = i - part * rows;
+        float top = kMinusInf;
+        for (int q = 0; q < parts; ++q) top = fmaxf(top, weights[q * ROWS + r]);
+        mine[k] = weight_of(weights[part * ROWS + r], top);
+        if (part == 0) tops[r] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kWeights; ++k) {
+        const int i = threadIdx.x + k * THREADS;
+        if (i >= parts * rows) break;
+        const int part = i / rows, r = i - part * rows;
+        weights[part * ROWS + r] = mine[k];
+    }
+    __syncthreads();
+    float4_t v[kSets];
+    float s[kSets];
+#pragma unroll
+    for (int k = 0; k < kSets; ++k) v[k] = float4_t{0.0f, 0.0f, 0.0f, 0.0f}, s[k] = 0.0f;
+    for (int p0 = 0; p0 < parts; p0 += kAhead) {
+        if (p0 > 0) load(p0);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (p0 + j >= parts) break;
+#pragma unroll
+            for (int k = 0; k < kSets; ++k) {
+                const int r = min(static_cast<int>(threadIdx.x + k * THREADS) / (D / 4), rows - 1);
+                const float w = weights[(p0 + j) * ROWS + r];
+                s[k] += w * sums[(p0 + j) * ROWS + r];
+                v[k] += w * x[j][k];
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kSets; ++k) {
+        const int of = threadIdx.x + k * THREADS;
+        if (of < rows * (D / 4)) sink(of / (D / 4), 4 * (of % (D / 4)), v[k], tops[of / (D / 4)], s[k]);
+    }
+    __syncthreads();       // (`scratch` is free again)
+}
 
 constexpr int kHeld = 2;             // tiles that a wavefront holds: the one at work, and those under way
 constexpr int kAttendWaves = 4;      // wavefronts of a workgroup; a step: one tile for each

@@ -1,4 +1,4 @@
-// Device code that the kernels of gqsa_cache.hip and gqsa_prompt.hip share.  Included by .hip files only, after the HIP runtime.
+// Device code that the kernels of the cache, of prompts and of verification share.  Included by .hip files only, after the HIP runtime.
 #pragma once
 
 #include "gqsa_attention.hpp"

@@ -1,6 +1,6 @@
 // Attention of a tree's rows over the 4-bit cache where a head of the cache has many rows (gqsa_cache_attend_tree; with few of them, the kernel of gqsa_cache_attend has it).
 //   s_j = scale q k_j for the tokens j before the rows and those of the rows that the mask names;   m = max s_j,   out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m)
-// in one pass over the tokens: maximum (as a reference that follows it from 2^7 below, see gqsa_cache.hip), sum and weighted sum go along in fp32, weights are rounded to
+// in one pass over the tokens: maximum (as a reference that follows it from 2^7 below, see kRoom in gqsa_device.hpp), sum and weighted sum go along in fp32, weights are rounded to
 // fp16 as the second product takes them, and their sum is of the rounded ones, so that the rounding of the largest weight cancels.
 //
 // What the kernel for few rows spends its time on is turning codes into numbers, anew for every 16 rows.  Here a workgroup of 8 wavefronts takes 128 rows of a
