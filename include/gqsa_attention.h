@@ -68,7 +68,8 @@ typedef struct {
     int32_t head_dim;
     int32_t token_bytes;        /* of one token and head: keys and values, codes, low and step */
     int64_t device_bytes;       /* pages */
-    int64_t workspace_bytes;    /* partial results of gqsa_cache_attend and gqsa_cache_attend_tree: about 34 MB with heads of 128, half of that with 64 */
+    int64_t workspace_bytes;    /* partial results of gqsa_cache_attend and gqsa_cache_attend_tree: 34 MB with heads of 128, 17 with 64, whatever the cache's size and whether trees
+                                   are attended to or not (gqsa_cache_attend alone would take 13 and 6.5).  Each handle has its own: 32 of them with heads of 128 1.1 GB */
 } gqsa_cache_info_t;
 
 /*
@@ -150,7 +151,11 @@ gqsa_status_t gqsa_cache_attend(gqsa_cache_t c, const void* q, int64_t q_row_str
  *   masks    [device] int32 [n_rows, mask_words]: bit j % 32 of word j / 32 stands for row j of the row's own sequence (bits of rows that it does not have, and rows
  *            from 32 mask_words on: not seen); mask_words 1 .. 2^15 (GQSA_ERR_UNSUPPORTED)
  * Keys and values that a row does not see have no effect on it, whatever they hold.  Rows that would be tokens beyond what the pages hold, which gqsa_cache_append leaves
- * out, are seen by nobody, and see what there is like any other.  The rest as in gqsa_cache_attend.
+ * out, are seen by nobody, and see what there is like any other.
+ * Which of two kernels runs hangs on what the host knows: max_pages and the mean number of rows, not the lengths.  With more than 32 rows (of a sequence times heads of a group) on average
+ * the one for many rows is taken where the table has much room.  Short sequences under a wide table are slower for it: 500 tokens, 64 rows for each of 8 heads 15.7 us with a table for
+ * 131072 tokens, 9.3 with one for 500; 16 x 1000 tokens, the same 27 and 20; so give no more pages than the longest sequence has where that is known.  One large tree among sequences of
+ * one row goes to the kernel for few: 32 x 4000 tokens, 32 heads for 8, one of 64 rows among 31 of one 41 us.  The rest as in gqsa_cache_attend.
  */
 gqsa_status_t gqsa_cache_attend_tree(gqsa_cache_t c, const void* q, int64_t q_row_stride, int64_t q_head_stride, int q_heads,
                                      int64_t n_rows, const int32_t* pages, int max_pages, const int32_t* lengths,

@@ -110,7 +110,7 @@ struct RotatedArgs {
 };
 
 // The append with its rotation: 8192 tokens of 32 query heads and 8 of the cache take 49 us (178 MB, 34 at the rate of a copy); norm and rotation, and append, in launches of
-// their own some 50 (34 and 16), and a launch more.  One token of 32 heads takes 5.7.  Bound: for prompts by the vector units, busy for 60 % of the cycles,
+// their own some 50 (34 and 16), and a launch more.  One token of 32 heads takes 5.5.  Bound: for prompts by the vector units, busy for 60 % of the cycles,
 // and memory (3.7 TB/s) in turn: the workgroups of the cache alone take 22 us, those of the queries alone 37, both without norms 45; for single tokens by the chain of waits
 // (lengths -> page -> rows and positions -> table -> LDS -> tile).  They come first in the grid: taken in turn
 // with those of the queries 64 us instead of 61 with the read.
